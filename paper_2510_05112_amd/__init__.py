@@ -6,8 +6,9 @@ reductions, top-k -- runs in the library's kernels.  PyTorch provides device
 memory and the stream, nothing else.  There is no CPU fallback: if the library
 is missing or no GPU is present, the device calls raise.
 """
+from . import stage_ops
 from .binding import (FLAG_DEADLOCK, FLAG_INCOMPLETE, FLAG_OVER_CAP, FpschedError, Problem,
                       library_path, load_library, version)
 
-__all__ = ["Problem", "FpschedError", "load_library", "library_path", "version",
+__all__ = ["Problem", "FpschedError", "load_library", "library_path", "version", "stage_ops",
            "FLAG_DEADLOCK", "FLAG_INCOMPLETE", "FLAG_OVER_CAP"]

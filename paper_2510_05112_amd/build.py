@@ -8,7 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfpsched.so")
-SOURCES = ["fpsched_api.hip", "eval_general.hip", "eval_sync.hip", "eval_slots.hip", "rows.hip", "timing.hip", "generate.hip", "topk.hip", "pareto.hip", "wslide.hip"]
+SOURCES = ["fpsched_api.hip", "eval_general.hip", "eval_sync.hip", "eval_slots.hip", "rows.hip", "timing.hip", "generate.hip", "topk.hip", "pareto.hip", "wslide.hip",
+           "op_embedding.hip", "op_recurrence.hip", "op_ffn.hip", "op_logprobs.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-command-line-argument"]
@@ -22,8 +23,8 @@ def stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [
-        os.path.join(os.path.dirname(HERE), "include", "fpsched.h")]
+    include = os.path.join(os.path.dirname(HERE), "include")
+    deps = [os.path.join(d, f) for d in (CSRC, include) for f in os.listdir(d)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -1,0 +1,390 @@
+// Gated feed-forward block:  [g u] = x w_in^T,  hidden = act(g) u,  out = hidden w_out^T, and its B and W items.
+//
+// All products go through one kernel on the matrix cores.  out[m][n] = sum over k of M(m, k) N(n, k); either operand lies in memory
+// with k running along its rows (kAlong) or down them (kDown):
+//   F:  x w_in^T (both along; both projections in one tile, act and product in its epilogue),  hidden w_out^T (both along)
+//   B:  grad w_out (N down; the derivative of the gate in its epilogue),  d_pre w_in (N down: one product over gate and up together)
+//   W:  d_pre^T x,  grad^T hidden (both down)
+// so that nothing is transposed in memory.  A tile of 64 k of either operand goes to LDS without passing registers, 16 bytes a lane;
+// what is past an operand's end arrives as zeros (buffer loads check the range), so that sizes need not fit tiles.  Of an operand
+// along k a lane reads its 8 k as they lie there; of one down k the transposing LDS read hands every lane 4 k of its column.  Pieces of 16 bytes are
+// placed crosswise (xor with the row) so that a read meets every bank once.
+//
+// The N operand is the matrix instruction's first, so that a lane holds four neighbouring n of one m, which is how rows are written.
+#include "ops_common.h"
+
+namespace fpsched {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T>
+struct Frag;
+template <>
+struct Frag<__bf16> {
+  typedef __bf16 type __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x16 mul(type a, type b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Frag<_Float16> {
+  typedef _Float16 type __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x16 mul(type a, type b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+
+enum { kAlong, kDown };                        // how k lies in an operand
+enum { kStore, kGated, kGatedGrad };           // what becomes of a tile
+constexpr int kDepth = 64;                     // k of a tile in LDS
+constexpr unsigned kOutside = 0x80000000u;     // an offset behind the end of every tile's buffer
+
+struct Operand {
+  const void* data;
+  int64_t stride;      // between rows, in elements
+  int64_t extent;      // m or n
+};
+
+struct Gemm {
+  Operand m, n;
+  int64_t depth;             // k
+  int64_t n_half;            // kGated, kGatedGrad: columns of the gate's half
+  void* out;
+  int64_t out_stride;
+  int accumulate;
+  int act;
+  void* pre;                 // kGated: written unless NULL; kGatedGrad: read
+  int tiles_m, tiles_n;
+};
+
+// ---- activations: the value, and with it the derivative ----------------------------------------------------------------
+
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + fast_exp(-x)); }
+
+constexpr float kGeluScale = 1.5957691216057308f, kGeluCube = 0.044715f;   // 2 sqrt(2 / pi); (1 + tanh y) / 2 = sigmoid(2 y)
+
+__device__ __forceinline__ float activate(int act, float g) {
+  if (act == FPSCHED_SILU) return g * sigmoid(g);
+  if (act == FPSCHED_GELU) return g * sigmoid(kGeluScale * (g + kGeluCube * g * g * g));
+  return fmaxf(g, 0.f);
+}
+__device__ __forceinline__ float slope(int act, float g) {
+  if (act == FPSCHED_RELU) return g > 0.f ? 1.f : 0.f;
+  const float c = fminf(fmaxf(g, -40.f), 40.f);   // (beyond, 0 or 1 to the last bit; squares would overflow)
+  if (act == FPSCHED_SILU) {
+    const float p = sigmoid(c);
+    return p * (1.f + c * (1.f - p));
+  }
+  const float p = sigmoid(kGeluScale * (c + kGeluCube * c * c * c));
+  return p + c * p * (1.f - p) * kGeluScale * (1.f + 3.f * kGeluCube * c * c);
+}
+
+// ---- tiles in LDS --------------------------------------------------------------------------------------------------------
+
+typedef __attribute__((address_space(3))) char lds_char;
+
+// A tile of ROWS m (or n) by kDepth k.  kAlong: [row][8 pieces of 8 k], piece p of row r in place p ^ (r / 2 % 8): of 16 rows that a read
+// takes one piece each, no two are in the same banks.  kDown: [k][ROWS / 8 pieces of 8 rows], piece p of k in place p ^ (k % 4 * 4): the
+// four k of a transposing read are in different quarters of the banks.
+template <int LAYOUT, int ROWS, int THREADS>
+struct Tile {
+  static constexpr int kBytes = ROWS * kDepth * 2, kLoads = kBytes / 16 / THREADS;
+
+  // The tile's part of an operand at rows `row0`, k `k0`, to LDS.  half: rows from ROWS / 2 on are those of another place, half_row0.
+  template <bool HALVES>
+  static __device__ __forceinline__ void load(const Operand& o, int64_t row0, int64_t half_row0, int64_t half_extent, int64_t k0, int64_t depth,
+                                              char* lds, int thread) {
+    const int wave = thread >> 6;
+    const int64_t k_left = min(depth - k0, (int64_t)kDepth);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int q = i * THREADS + thread;
+      unsigned offset;
+      const char* base;
+      int64_t bytes;
+      if constexpr (LAYOUT == kAlong) {
+        constexpr int kRows = HALVES ? ROWS / 2 : ROWS, kRowsOfLoad = THREADS / 8;
+        static_assert(kRows % kRowsOfLoad == 0, "a load is in one half");
+        const int r = q >> 3, piece = (q & 7) ^ (r >> 1 & 7);
+        const bool second = i * kRowsOfLoad >= kRows;   // (a constant)
+        const int64_t first = second ? half_row0 : row0, end = HALVES && !second ? half_extent : o.extent;
+        const int64_t rows = max(min(end - first, (int64_t)kRows), (int64_t)0);
+        base = static_cast<const char*>(o.data) + (first * o.stride + k0) * 2;
+        bytes = rows > 0 ? ((rows - 1) * o.stride + k_left) * 2 : 0;
+        offset = (unsigned)((second ? r - kRows : r) * (int)o.stride + piece * 8) * 2;
+        if (piece * 8 >= k_left) offset = kOutside;
+      } else {
+        constexpr int kPieces = ROWS / 8;
+        const int k = q / kPieces, piece = (q % kPieces) ^ ((k & 3) << 2);
+        const int64_t left = o.extent - row0;
+        base = static_cast<const char*>(o.data) + (k0 * o.stride + row0) * 2;
+        bytes = ((k_left - 1) * o.stride + left) * 2;
+        offset = (unsigned)(k * (int)o.stride + piece * 8) * 2;
+        if (piece * 8 >= left) offset = kOutside;
+      }
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)min(bytes, (int64_t)0x7fffffff), 0x00027000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_char*)(lds + (i * THREADS + wave * 64) * 16), 16, (int)offset, 0, 0, 0);
+    }
+  }
+
+  // A lane's 8 k (16 step + 8 (lane / 32) ...) of row first + lane % 32.
+  template <typename T>
+  static __device__ __forceinline__ typename Frag<T>::type frag(const char* lds, int first, int step, int lane) {
+    if constexpr (LAYOUT == kAlong) {
+      const int r = first + (lane & 31), piece = step * 2 + (lane >> 5);
+      return *reinterpret_cast<const typename Frag<T>::type*>(lds + r * (kDepth * 2) + ((piece ^ (r >> 1 & 7)) << 4));
+    } else {
+      const int k = step * 16 + (lane >> 5) * 8 + (lane >> 2 & 3), column = first + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+      const int place = ((column >> 3) ^ ((k & 3) << 2)) * 16 + (column & 7) * 2;
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + k * (ROWS * 2) + place));
+      const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + (k + 4) * (ROWS * 2) + place));
+      const s16x8 both = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
+      return __builtin_bit_cast(typename Frag<T>::type, both);
+    }
+  }
+};
+
+// Tiles in an order in which those of one XCD (every eighth workgroup) are neighbours, eight rows of tiles high, for its L2.
+__device__ __forceinline__ void tile_of(unsigned id, int tiles_m, int tiles_n, int* tm, int* tn) {
+  const unsigned all = (unsigned)tiles_m * tiles_n, each = all >> 3, more = all & 7, xcd = id & 7, at = id >> 3;
+  const unsigned place = xcd * each + min(xcd, more) + at;
+  const unsigned strip = place / (8u * tiles_n), in = place - strip * 8u * tiles_n;
+  const unsigned high = min(8u, tiles_m - strip * 8u);
+  *tm = strip * 8 + in % high;
+  *tn = in / high;
+}
+
+template <typename T, int LM, int LN, int EPILOGUE, typename O, int BM, int BN>
+__global__ __launch_bounds__(BN * 2) void gemm_kernel(Gemm a) {
+  constexpr int kThreads = BN * 2;                         // (a wavefront for 64 columns of half of the rows)
+  constexpr int kWavesN = BN / 64, MF = BM / 64, NF = 2;
+  using TileM = Tile<LM, BM, kThreads>;
+  using TileN = Tile<LN, BN, kThreads>;
+  constexpr bool kHalves = EPILOGUE == kGated;
+  __shared__ __align__(1024) char lds[2][TileM::kBytes + TileN::kBytes];
+  const int thread = threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+  const int wave_m = wave / kWavesN, wave_n = wave % kWavesN;
+  int tm, tn;
+  tile_of(blockIdx.x, a.tiles_m, a.tiles_n, &tm, &tn);
+  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * (kHalves ? BN / 2 : BN);
+  f32x16 acc[MF][NF] = {};
+  auto load = [&](int64_t k0, char* to) {
+    TileM::template load<false>(a.m, m0, 0, 0, k0, a.depth, to, thread);
+    TileN::template load<kHalves>(a.n, n0, a.n_half + n0, a.n_half, k0, a.depth, to + TileM::kBytes, thread);
+  };
+  load(0, lds[0]);
+  int buffer = 0;
+  for (int64_t k0 = 0; k0 < a.depth; k0 += kDepth, buffer ^= 1) {
+    __syncthreads();   // this tile has arrived, and the other buffer's has been read
+    if (k0 + kDepth < a.depth) load(k0 + kDepth, lds[buffer ^ 1]);
+    const char *at_m = lds[buffer], *at_n = lds[buffer] + TileM::kBytes;
+#pragma unroll
+    for (int step = 0; step < kDepth / 16; ++step) {
+      typename Frag<T>::type fm[MF], fn[NF];
+#pragma unroll
+      for (int i = 0; i < MF; ++i) fm[i] = TileM::template frag<T>(at_m, (wave_m * MF + i) * 32, step, lane);
+#pragma unroll
+      for (int j = 0; j < NF; ++j) fn[j] = TileN::template frag<T>(at_n, kHalves ? j * (BN / 2) + wave_n * 32 : (wave_n * NF + j) * 32, step, lane);
+#pragma unroll
+      for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = Frag<T>::mul(fn[j], fm[i], acc[i][j]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MF; ++i) {
+    const int64_t m = m0 + (wave_m * MF + i) * 32 + (lane & 31);
+    if (m >= a.m.extent) continue;
+    if constexpr (EPILOGUE == kGated) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t f = n0 + wave_n * 32 + q * 8 + (lane >> 5) * 4;   // (a multiple of 4, as is their number)
+        if (f >= a.n_half) continue;
+        Vec<T, 4> h, g, u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float gate = acc[i][0][q * 4 + e], up = acc[i][1][q * 4 + e];
+          h.at[e] = (T)(activate(a.act, gate) * up);
+          g.at[e] = (T)gate;
+          u.at[e] = (T)up;
+        }
+        store_vec<T, 4>(static_cast<T*>(a.out) + m * a.out_stride + f, h);
+        if (a.pre) {
+          T* pre = static_cast<T*>(a.pre) + m * 2 * a.n_half + f;
+          store_vec<T, 4>(pre, g);
+          store_vec<T, 4>(pre + a.n_half, u);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NF; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t n = n0 + (wave_n * NF + j) * 32 + q * 8 + (lane >> 5) * 4;
+          if (n >= a.n.extent) continue;
+          if constexpr (EPILOGUE == kGatedGrad) {
+            const T* pre = static_cast<const T*>(a.pre) + m * 2 * a.n_half + n;
+            const Vec<T, 4> g = load_vec<T, 4>(pre), u = load_vec<T, 4>(pre + a.n_half);
+            Vec<T, 4> dg, du;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float d = acc[i][j][q * 4 + e], gate = (float)g.at[e];
+              dg.at[e] = (T)(d * (float)u.at[e] * slope(a.act, gate));
+              du.at[e] = (T)(d * activate(a.act, gate));
+            }
+            T* out = static_cast<T*>(a.out) + m * a.out_stride + n;
+            store_vec<T, 4>(out, dg);
+            store_vec<T, 4>(out + a.n_half, du);
+          } else {
+            O* out = static_cast<O*>(a.out) + m * a.out_stride + n;
+            Vec<O, 4> v = {};
+            if (std::is_same<O, float>::value && a.accumulate) v = load_vec<O, 4>(out);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v.at[e] = (O)((float)v.at[e] + acc[i][j][q * 4 + e]);
+            store_vec<O, 4>(out, v);
+          }
+        }
+    }
+  }
+}
+
+// A product of nothing: the zeros that it leaves.
+template <typename O>
+__global__ __launch_bounds__(256) void zero_rows_kernel(O* out, int64_t stride, int64_t rows, int64_t columns) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * columns; i += (int64_t)gridDim.x * 256)
+    out[i / columns * stride + i % columns] = (O)0.f;
+}
+
+// Tiles of 256 x 256 where there are enough of them to go round the compute units, else of 128 x 128.
+template <typename T, int LM, int LN, int EPILOGUE, typename O>
+int gemm(Gemm a, hipStream_t stream) {
+  const int64_t columns = EPILOGUE == kGated ? 2 * a.n_half : a.n.extent;
+  auto go = [&](auto size) {
+    constexpr int B = decltype(size)::value;
+    const int64_t tm = ceil_div(a.m.extent, B), tn = ceil_div(columns, B);
+    if (tm * tn > 0x7fffffff) return (int)FPSCHED_EINVAL;
+    a.tiles_m = (int)tm;
+    a.tiles_n = (int)tn;
+    gemm_kernel<T, LM, LN, EPILOGUE, O, B, B><<<dim3((unsigned)(tm * tn)), dim3(B * 2), 0, stream>>>(a);
+    return launched();
+  };
+  if (ceil_div(a.m.extent, 256) * ceil_div(columns, 256) >= 160) return go(std::integral_constant<int, 256>());
+  return go(std::integral_constant<int, 128>());
+}
+
+constexpr int64_t kMostStride = 1 << 21;   // (256 rows of a tile are within 2^31 bytes)
+
+bool row_ok(const void* p, int64_t stride) { return p && aligned(p, 16) && stride % 8 == 0 && stride <= kMostStride; }
+
+int check_sizes(int type, int act, int64_t n_tokens, int64_t width, int64_t hidden_width) {
+  if (type != FPSCHED_BF16 && type != FPSCHED_F16) return FPSCHED_EINVAL;
+  if (act < FPSCHED_SILU || act > FPSCHED_RELU || n_tokens < 0 || n_tokens > 0x7fffffffll) return FPSCHED_EINVAL;
+  if (width < 8 || hidden_width < 8 || width % 8 || hidden_width % 8 || width > kMostStride || hidden_width > kMostStride / 2) return FPSCHED_EINVAL;
+  return FPSCHED_OK;
+}
+
+template <typename F>
+int with_half_type(int type, F f) {
+  return type == FPSCHED_BF16 ? f(__bf16()) : f(_Float16());
+}
+
+}  // namespace
+}  // namespace fpsched
+
+using namespace fpsched;
+
+extern "C" {
+
+size_t fpsched_op_ffn_workspace_bytes(int64_t n_tokens, int64_t width, int64_t hidden_width) {
+  if (check_sizes(FPSCHED_BF16, 0, n_tokens, width, hidden_width) != FPSCHED_OK) return 0;
+  return 16;
+}
+
+int fpsched_op_ffn(int device_id, int type, int act, int64_t n_tokens, int64_t width, int64_t hidden_width, const void* x,
+                   int64_t x_stride, const void* w_in, const void* w_out, void* pre, void* hidden, void* out, int64_t out_stride,
+                   void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  if (check_sizes(type, act, n_tokens, width, hidden_width) != FPSCHED_OK || x_stride < width || out_stride < width) return FPSCHED_EINVAL;
+  if (device_id < 0) return FPSCHED_ENODEV;
+  if (n_tokens == 0) return FPSCHED_OK;
+  if (!row_ok(x, x_stride) || !row_ok(out, out_stride) || !row_ok(w_in, 0) || !row_ok(w_out, 0) || !row_ok(hidden, 0) || (pre && !aligned(pre, 16)))
+    return FPSCHED_EINVAL;
+  OpsDevice g(device_id);
+  if (!g.ok) return FPSCHED_EHIP;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  return with_half_type(type, [&](auto zero) {
+    using T = decltype(zero);
+    Gemm a = {};
+    a.m = {x, x_stride, n_tokens}; a.n = {w_in, width, 2 * hidden_width}; a.depth = width; a.n_half = hidden_width;
+    a.out = hidden; a.out_stride = hidden_width; a.act = act; a.pre = pre;
+    const int first = gemm<T, kAlong, kAlong, kGated, T>(a, stream);
+    if (first != FPSCHED_OK) return first;
+    Gemm b = {};
+    b.m = {hidden, hidden_width, n_tokens}; b.n = {w_out, hidden_width, width}; b.depth = hidden_width;
+    b.out = out; b.out_stride = out_stride;
+    return gemm<T, kAlong, kAlong, kStore, T>(b, stream);
+  });
+}
+
+int fpsched_op_ffn_input_grad(int device_id, int type, int act, int64_t n_tokens, int64_t width, int64_t hidden_width,
+                              const void* grad, int64_t grad_stride, const void* w_in, const void* w_out, const void* pre,
+                              void* d_pre, void* d_x, int64_t d_x_stride, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  if (check_sizes(type, act, n_tokens, width, hidden_width) != FPSCHED_OK || grad_stride < width || d_x_stride < width) return FPSCHED_EINVAL;
+  if (device_id < 0) return FPSCHED_ENODEV;
+  if (n_tokens == 0) return FPSCHED_OK;
+  if (!row_ok(grad, grad_stride) || !row_ok(d_x, d_x_stride) || !row_ok(w_in, 0) || !row_ok(w_out, 0) || !row_ok(pre, 0) || !row_ok(d_pre, 0))
+    return FPSCHED_EINVAL;
+  OpsDevice g(device_id);
+  if (!g.ok) return FPSCHED_EHIP;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  return with_half_type(type, [&](auto zero) {
+    using T = decltype(zero);
+    Gemm a = {};
+    a.m = {grad, grad_stride, n_tokens}; a.n = {w_out, hidden_width, hidden_width}; a.depth = width; a.n_half = hidden_width;
+    a.out = d_pre; a.out_stride = 2 * hidden_width; a.act = act; a.pre = const_cast<void*>(pre);
+    const int first = gemm<T, kAlong, kDown, kGatedGrad, T>(a, stream);
+    if (first != FPSCHED_OK) return first;
+    Gemm b = {};
+    b.m = {d_pre, 2 * hidden_width, n_tokens}; b.n = {w_in, width, width}; b.depth = 2 * hidden_width;
+    b.out = d_x; b.out_stride = d_x_stride;
+    return gemm<T, kAlong, kDown, kStore, T>(b, stream);
+  });
+}
+
+int fpsched_op_ffn_weight_grad(int device_id, int type, int64_t n_tokens, int64_t width, int64_t hidden_width, const void* x,
+                               int64_t x_stride, const void* grad, int64_t grad_stride, const void* hidden, const void* d_pre,
+                               int out_type, void* d_w_in, void* d_w_out, int accumulate, void* d_workspace,
+                               size_t workspace_bytes, void* hip_stream) {
+  if (check_sizes(type, 0, n_tokens, width, hidden_width) != FPSCHED_OK || x_stride < width || grad_stride < width) return FPSCHED_EINVAL;
+  if ((out_type != type && out_type != FPSCHED_F32) || (accumulate && out_type != FPSCHED_F32)) return FPSCHED_EINVAL;
+  if (device_id < 0) return FPSCHED_ENODEV;
+  if (!row_ok(d_w_in, 0) || !row_ok(d_w_out, 0)) return FPSCHED_EINVAL;
+  if (n_tokens > 0 && (!row_ok(x, x_stride) || !row_ok(grad, grad_stride) || !row_ok(hidden, 0) || !row_ok(d_pre, 0))) return FPSCHED_EINVAL;
+  if (n_tokens == 0 && accumulate) return FPSCHED_OK;
+  OpsDevice g(device_id);
+  if (!g.ok) return FPSCHED_EHIP;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  return with_half_type(type, [&](auto zero) {
+    using T = decltype(zero);
+    auto go = [&](auto zero_out) {
+      using O = decltype(zero_out);
+      if (n_tokens == 0) {
+        zero_rows_kernel<O><<<dim3(1024), dim3(256), 0, stream>>>(static_cast<O*>(d_w_in), width, 2 * hidden_width, width);
+        zero_rows_kernel<O><<<dim3(1024), dim3(256), 0, stream>>>(static_cast<O*>(d_w_out), hidden_width, width, hidden_width);
+        return launched();
+      }
+      Gemm a = {};
+      a.m = {d_pre, 2 * hidden_width, 2 * hidden_width}; a.n = {x, x_stride, width}; a.depth = n_tokens;
+      a.out = d_w_in; a.out_stride = width; a.accumulate = accumulate;
+      const int first = gemm<T, kDown, kDown, kStore, O>(a, stream);
+      if (first != FPSCHED_OK) return first;
+      Gemm b = {};
+      b.m = {grad, grad_stride, width}; b.n = {hidden, hidden_width, hidden_width}; b.depth = n_tokens;
+      b.out = d_w_out; b.out_stride = hidden_width; b.accumulate = accumulate;
+      return gemm<T, kDown, kDown, kStore, O>(b, stream);
+    };
+    if (out_type == FPSCHED_F32) return go(float());
+    return go(T());
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,385 @@
+// Log probabilities of given tokens, the entropy and the likeliest alternatives, in one pass over the logits, and the gradient.
+//
+// With m the largest logit of what was seen, s = sum e^(x - m) and w = sum e^(x - m) (x - m), what is asked for is
+//   log p[token] = (x[token] - m) - log s,   entropy = log s - w / s,
+// and two parts of a row are put together by multiplying s by e^(m1 - m) and adding s (m1 - m) to w.  A lane looks at 16
+// bytes of logits at a time and changes its m only where one of them is larger.  Rows are cut into parts where there are fewer rows than
+// the chip has room for; a second kernel puts the parts together.
+//
+// Alternatives: a wavefront keeps its logits of the part in registers, every lane names its best, and k times the best of
+// those is taken and its lane names the next one (logits are compared as integers in their order, with the id behind, so that equal ones come by ascending id).
+//
+// Masked logits are minus infinity, and x - m = -infinity gives e = 0, but 0 times it is NaN: factors are held at -1000.  m begins at the
+// type's lowest number and not at minus infinity, so that a row of masks needs no branch: its s stays 0.
+//
+// Gradient: one pass, element by element, bound by memory.
+#include "ops_common.h"
+
+#include <float.h>
+
+namespace fpsched {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMostAlternatives = 32;
+constexpr int kHeld = 64;                              // logits a lane keeps for the alternatives
+constexpr int64_t kHeldPart = (int64_t)kThreads * kHeld;
+
+__device__ __forceinline__ float held_back(float x) { return x < -1000.f ? -1000.f : x; }   // (NaN stays)
+
+struct Stats {
+  float m, s, w;
+
+  __device__ __forceinline__ void raise(float to) {
+    const float d = held_back(m - to), f = fast_exp(d);
+    w = f * (w + s * d);
+    s *= f;
+    m = to;
+  }
+  __device__ __forceinline__ void add(float x) {   // x <= m, or not a number
+    const float e = fast_exp(x - m);
+    s += e;
+    w += e * held_back(x - m);
+  }
+  __device__ __forceinline__ void join(const Stats& o) {
+    const float most = fmaxf(m, o.m);
+    Stats other = o;
+    raise(most);
+    other.raise(most);
+    s += other.s;
+    w += other.w;
+  }
+};
+
+__device__ __forceinline__ Stats nothing() { return {-FLT_MAX, 0.f, 0.f}; }
+
+__device__ __forceinline__ Stats wave_stats(Stats a) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    Stats o;
+    o.m = __shfl_xor(a.m, d);
+    o.s = __shfl_xor(a.s, d);
+    o.w = __shfl_xor(a.w, d);
+    a.join(o);
+  }
+  return a;
+}
+
+// A logit and its id as one number: larger for a larger logit, then for a smaller id.  0: none.
+__device__ __forceinline__ unsigned long long ranked(float x, unsigned id) {
+  const unsigned bits = __float_as_uint(x), order = bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+  return (unsigned long long)order << 32 | (unsigned)~id;
+}
+__device__ __forceinline__ float logit_of(unsigned long long r) {
+  const unsigned order = (unsigned)(r >> 32);
+  return __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
+}
+__device__ __forceinline__ unsigned long long wave_most(unsigned long long a) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    const unsigned long long o = __shfl_xor(a, d);
+    a = o > a ? o : a;
+  }
+  return a;
+}
+
+struct PartOut {          // [row][part]
+  Stats* stats;
+  unsigned long long* best;   // [row][part][k], descending
+  int parts;
+};
+
+// -0 and 0 are equal logits
+template <typename T>
+__device__ __forceinline__ float logit(T x) { return (float)x + 0.f; }
+
+template <typename T>
+struct RowOut {
+  const T* logits;
+  int64_t stride, vocab;
+  const void* tokens;
+  int tokens64, k;
+  float *logprob, *entropy, *lse;
+  int32_t* ids;
+  float* alternatives;
+
+  // what lane 0 of a row's last wavefront writes
+  __device__ __forceinline__ void put(int64_t row, const Stats& a) const {
+    const int64_t token = token_at(tokens, tokens64, row);
+    const float ln = fast_log(a.s);
+    const bool none = a.s == 0.f;
+    float lp = 0.f;
+    if (token >= 0 && token < vocab) lp = none ? -INFINITY : (logit(logits[row * stride + token]) - a.m) - ln;
+    logprob[row] = a.s != a.s ? a.s : lp;
+    entropy[row] = none ? 0.f : ln - a.w / a.s;
+    lse[2 * row] = none ? 0.f : a.m;
+    lse[2 * row + 1] = none ? -INFINITY : ln;
+  }
+  __device__ __forceinline__ void put_alternative(int64_t row, int i, unsigned long long r, const Stats& a) const {
+    const float x = logit_of(r);
+    const bool masked = r == 0 || x == -INFINITY, wrong = a.s != a.s;
+    ids[row * k + i] = masked || wrong ? -1 : (int32_t)~(unsigned)r;
+    alternatives[row * k + i] = wrong ? a.s : masked ? -INFINITY : (x - a.m) - fast_log(a.s);
+  }
+};
+
+// One part of a row.  blockIdx.x: row * parts + part.  ALT: with alternatives, of at most kHeldPart logits.
+template <typename T, bool ALT>
+__global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
+  constexpr int N = kWide<T>;
+  __shared__ Stats wave_sums[kWaves];
+  __shared__ unsigned long long wave_best[kWaves][kMostAlternatives];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = row_out.k;
+  const int64_t row = blockIdx.x / part_out.parts, part = blockIdx.x % part_out.parts;
+  const T* logits = row_out.logits + row * row_out.stride;
+  // pieces of 16 bytes that are aligned as such, the first and the last one cut off at the part's ends
+  const int64_t begin = part * part_length, end = min(begin + part_length, row_out.vocab);
+  const int64_t skew = (int64_t)((reinterpret_cast<uintptr_t>(logits + begin) & 15) / sizeof(T));
+  Stats mine = nothing();
+  constexpr int kPieces = kHeld / N + 1;   // (a piece more, since the first begins in front of the part)
+  Vec<T, N> held[ALT ? kPieces : 1];
+  auto get = [&](int64_t at, T none) {     // logits at .. at + N - 1
+    Vec<T, N> v;
+    if (at >= begin && at + N <= end) {
+      v = load_vec<T, N>(logits + at);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v.at[i] = at + i >= begin && at + i < end ? logits[at + i] : none;
+    }
+    return v;
+  };
+  auto take = [&](const Vec<T, N>& v) {
+    float x[N], most = -FLT_MAX;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] = (float)v.at[i];
+      most = fmaxf(most, x[i]);
+    }
+    if (most > mine.m) mine.raise(most);
+#pragma unroll
+    for (int i = 0; i < N; ++i) mine.add(x[i]);
+  };
+  const int64_t first = begin - skew + (int64_t)threadIdx.x * N;
+  if constexpr (ALT) {
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) held[p] = get(first + (int64_t)p * kThreads * N, (T)-INFINITY);
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) take(held[p]);
+  } else {
+    constexpr int kAhead = 4;
+    for (int64_t at = first; at < end; at += kAhead * kThreads * N) {
+      Vec<T, N> v[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) v[i] = get(at + (int64_t)i * kThreads * N, (T)-INFINITY);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) take(v[i]);
+    }
+  }
+  const Stats sums = wave_stats(mine);
+  if (lane == 0) wave_sums[wave] = sums;
+  if constexpr (ALT) {
+    // the lane's best below `bar`
+    auto next = [&](unsigned long long bar) {
+      unsigned long long best = 0;
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) {
+        const int64_t at = first + (int64_t)p * kThreads * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const unsigned long long r = at + i >= begin && at + i < end ? ranked(logit(held[p].at[i]), (unsigned)(at + i)) : 0;
+          if (r < bar && r > best) best = r;
+        }
+      }
+      return best;
+    };
+    unsigned long long best = next(~0ull);
+    for (int i = 0; i < k; ++i) {
+      const unsigned long long most = wave_most(best);
+      if (lane == 0) wave_best[wave][i] = most;
+      if (best == most && most) best = next(most);
+    }
+  }
+  __syncthreads();
+  if (wave) return;
+  Stats all = wave_sums[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) all.join(wave_sums[w]);
+  const bool whole = part_out.parts == 1;
+  const int64_t at = row * part_out.parts + part;
+  if (lane == 0) {
+    if (whole) row_out.put(row, all);
+    else part_out.stats[at] = all;
+  }
+  if constexpr (ALT) {
+    unsigned long long mine_of[kWaves * kMostAlternatives / 64];
+#pragma unroll
+    for (int j = 0; j < kWaves * kMostAlternatives / 64; ++j) {
+      const int n = j * 64 + lane;
+      mine_of[j] = n < kWaves * k ? wave_best[n / k][n % k] : 0;
+    }
+    for (int i = 0; i < k; ++i) {
+      unsigned long long best = 0;
+#pragma unroll
+      for (int j = 0; j < kWaves * kMostAlternatives / 64; ++j) best = mine_of[j] > best ? mine_of[j] : best;
+      best = wave_most(best);
+#pragma unroll
+      for (int j = 0; j < kWaves * kMostAlternatives / 64; ++j)
+        if (mine_of[j] == best) mine_of[j] = 0;
+      if (lane == 0) {
+        if (whole) row_out.put_alternative(row, i, best, all);
+        else part_out.best[at * k + i] = best;
+      }
+    }
+  }
+}
+
+// The parts of a row put together, a wavefront a row.
+template <typename T>
+__global__ __launch_bounds__(64) void logprobs_join_kernel(RowOut<T> row_out, PartOut part_out) {
+  const int lane = threadIdx.x, k = row_out.k;
+  const int64_t row = blockIdx.x;
+  Stats mine = nothing();
+  for (int p = lane; p < part_out.parts; p += 64) mine.join(part_out.stats[row * part_out.parts + p]);
+  mine = wave_stats(mine);
+  if (lane == 0) row_out.put(row, mine);
+  const unsigned long long* best = part_out.best + row * part_out.parts * k;
+  unsigned long long bar = ~0ull;
+  for (int i = 0; i < k; ++i) {
+    unsigned long long most = 0;
+    for (int n = lane; n < part_out.parts * k; n += 64) {
+      const unsigned long long r = best[n];
+      if (r < bar && r > most) most = r;
+    }
+    bar = wave_most(most);
+    if (lane == 0) row_out.put_alternative(row, i, bar, mine);
+  }
+}
+
+template <typename T, int N>
+__global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(const T* logits, int64_t stride, int64_t vocab, const void* tokens,
+                                                                int tokens64, const float* lse, const float* entropy,
+                                                                const float* grad_logprob, const float* grad_entropy, T* out,
+                                                                int64_t out_stride, int pieces) {
+  const int64_t row = blockIdx.x / pieces;
+  const int64_t token = token_at(tokens, tokens64, row);
+  const bool given = token >= 0 && token < vocab;
+  const float m = lse[2 * row], ln = lse[2 * row + 1];
+  const float gl = given && grad_logprob ? grad_logprob[row] : 0.f, ge = grad_entropy ? grad_entropy[row] : 0.f, h = entropy[row];
+  const T* from = logits + row * stride;
+  T* to = out + row * out_stride;
+  const bool none = ln == -INFINITY;
+  auto gradient = [&](T x, int64_t i) {
+    const float lp = ((float)x - m) - ln;
+    const float p = fast_exp(lp);
+    const float d = (i == token ? gl : 0.f) - p * (gl + ge * (held_back(lp) + h));
+    return (T)(none ? 0.f : d);
+  };
+  constexpr int kRounds = 4;
+  const int64_t first = ((int64_t)(blockIdx.x % pieces) * kRounds * kThreads + threadIdx.x) * N;
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int64_t c = first + (int64_t)r * kThreads * N;
+    if (c + N <= vocab) {
+      Vec<T, N> v = load_vec<T, N>(from + c);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v.at[i] = gradient(v.at[i], c + i);
+      store_vec<T, N>(to + c, v);
+    } else {
+      for (int64_t i = c; i < vocab; ++i) to[i] = gradient(from[i], i);
+    }
+  }
+}
+
+struct Parts {
+  int64_t length;
+  int parts;
+};
+
+// Parts of a row: with alternatives what a workgroup's registers hold, fewer logits where there are few rows (1,024 workgroups
+// fill the chip), but 4,096 at least.
+Parts parts_of(int64_t n_rows, int64_t vocab, int k) {
+  const int64_t wanted = std::max<int64_t>(1, ceil_div(1024, std::max<int64_t>(1, n_rows)));
+  int64_t length = std::max<int64_t>(4096, ceil_div(vocab, wanted));
+  if (k > 0) length = std::min<int64_t>(length, kHeldPart);
+  length = (int64_t)round_up((size_t)length, 64);
+  Parts p;
+  p.length = length;
+  p.parts = (int)std::max<int64_t>(1, ceil_div(vocab, length));
+  return p;
+}
+
+bool sizes_fit(int64_t n_rows, int64_t vocab, int k) {
+  if (n_rows < 0 || n_rows > 0x7fffffffll || vocab < 1 || vocab > 0x7fffffffll || k < 0 || k > kMostAlternatives) return false;
+  return n_rows * parts_of(n_rows, vocab, k).parts <= 0x7fffffffll;
+}
+
+}  // namespace
+}  // namespace fpsched
+
+using namespace fpsched;
+
+extern "C" {
+
+size_t fpsched_op_logprobs_workspace_bytes(int64_t n_rows, int64_t vocab, int n_alternatives) {
+  if (!sizes_fit(n_rows, vocab, n_alternatives)) return 0;
+  const Parts p = parts_of(n_rows, vocab, n_alternatives);
+  if (p.parts == 1) return 16;
+  return round_up((size_t)n_rows * p.parts * sizeof(Stats), 16) + (size_t)n_rows * p.parts * n_alternatives * 8;
+}
+
+int fpsched_op_logprobs(int device_id, int type, int64_t n_rows, int64_t vocab, const void* logits, int64_t logits_stride,
+                        const void* tokens, int tokens64, int n_alternatives, float* logprob, float* entropy, float* lse,
+                        int32_t* ids, float* alternatives, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  if (type < FPSCHED_BF16 || type > FPSCHED_F32 || !sizes_fit(n_rows, vocab, n_alternatives) || logits_stride < vocab) return FPSCHED_EINVAL;
+  if (device_id < 0) return FPSCHED_ENODEV;
+  if (n_rows == 0) return FPSCHED_OK;
+  if (!logits || !tokens || !logprob || !entropy || !lse || (n_alternatives > 0 && (!ids || !alternatives))) return FPSCHED_EINVAL;
+  if (!aligned(logits, type == FPSCHED_F32 ? 4 : 2)) return FPSCHED_EINVAL;
+  const Parts p = parts_of(n_rows, vocab, n_alternatives);
+  if (p.parts > 1) {
+    if (!d_workspace || !aligned(d_workspace, 16)) return FPSCHED_EINVAL;
+    if (workspace_bytes < fpsched_op_logprobs_workspace_bytes(n_rows, vocab, n_alternatives)) return FPSCHED_ENOMEM;
+  }
+  OpsDevice g(device_id);
+  if (!g.ok) return FPSCHED_EHIP;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  return with_type(type, [&](auto zero) {
+    using T = decltype(zero);
+    const RowOut<T> row{static_cast<const T*>(logits), logits_stride, vocab, tokens, tokens64, n_alternatives, logprob, entropy, lse, ids, alternatives};
+    PartOut part{static_cast<Stats*>(d_workspace), nullptr, p.parts};
+    if (p.parts > 1)
+      part.best = reinterpret_cast<unsigned long long*>(static_cast<char*>(d_workspace) + round_up((size_t)n_rows * p.parts * sizeof(Stats), 16));
+    const dim3 grid((unsigned)(n_rows * p.parts));
+    if (n_alternatives > 0) logprobs_kernel<T, true><<<grid, dim3(kThreads), 0, stream>>>(row, part, p.length);
+    else logprobs_kernel<T, false><<<grid, dim3(kThreads), 0, stream>>>(row, part, p.length);
+    if (p.parts > 1) logprobs_join_kernel<T><<<dim3((unsigned)n_rows), dim3(64), 0, stream>>>(row, part);
+    return launched();
+  });
+}
+
+int fpsched_op_logprobs_grad(int device_id, int type, int64_t n_rows, int64_t vocab, const void* logits, int64_t logits_stride,
+                             const void* tokens, int tokens64, const float* lse, const float* entropy, const float* grad_logprob,
+                             const float* grad_entropy, void* out, int64_t out_stride, void* hip_stream) {
+  if (type < FPSCHED_BF16 || type > FPSCHED_F32 || !sizes_fit(n_rows, vocab, 0) || logits_stride < vocab || out_stride < vocab) return FPSCHED_EINVAL;
+  if (device_id < 0) return FPSCHED_ENODEV;
+  if (n_rows == 0) return FPSCHED_OK;
+  if (!logits || !tokens || !lse || !entropy || !out || (out == logits && out_stride != logits_stride)) return FPSCHED_EINVAL;
+  OpsDevice g(device_id);
+  if (!g.ok) return FPSCHED_EHIP;
+  return with_type(type, [&](auto zero) {
+    using T = decltype(zero);
+    auto go = [&](auto n) {
+      constexpr int N = decltype(n)::value;
+      const int64_t pieces = ceil_div(vocab, 4 * kThreads * N);
+      if (n_rows * pieces > 0x7fffffffll) return (int)FPSCHED_EINVAL;
+      logprobs_grad_kernel<T, N><<<dim3((unsigned)(n_rows * pieces)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
+          static_cast<const T*>(logits), logits_stride, vocab, tokens, tokens64, lse, entropy, grad_logprob, grad_entropy, static_cast<T*>(out),
+          out_stride, (int)pieces);
+      return launched();
+    };
+    if (wide_rows(logits, logits_stride, sizeof(T)) && wide_rows(out, out_stride, sizeof(T))) return go(std::integral_constant<int, kWide<T>>());
+    return go(std::integral_constant<int, 1>());
+  });
+}
+
+}  // extern "C"

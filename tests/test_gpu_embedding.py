@@ -1,0 +1,131 @@
+"""Embedding lookup and its gradient against the plain forms in 64 bits."""
+import pytest
+import torch
+
+import paper_2510_05112_amd as fp
+import stage_oracle as oracle
+
+pytestmark = pytest.mark.gpu
+ops = fp.stage_ops
+TYPES = [torch.bfloat16, torch.float16, torch.float32]
+
+
+def tokens_of(n, rows, seed, repeat=0.3):
+    """Tokens of which some repeat often, with paddings and one behind the table."""
+    g = torch.Generator().manual_seed(seed)
+    t = torch.randint(0, max(rows, 1), (n,), generator=g)
+    common = torch.randint(0, max(rows, 1), (2,), generator=g)
+    often = torch.rand(n, generator=g)
+    t = torch.where(often < repeat, common[0], t)
+    t = torch.where((often >= repeat) & (often < 1.3 * repeat), common[1], t)
+    t[torch.rand(n, generator=g) < 0.05] = -1
+    if n > 3:
+        t[n // 2] = rows
+    return t
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,rows,width", [(1, 1, 1), (61, 1000, 264), (7, 50, 33), (300, 17, 1024), (5, 1000, 4097), (2049, 70000, 8)])
+def test_lookup(dtype, n, rows, width):
+    g = torch.Generator().manual_seed(n)
+    table = torch.randn(rows, width, generator=g).to(dtype)
+    for wide in (torch.int32, torch.int64):
+        tokens = tokens_of(n, rows, n + 1).to(wide)
+        got = ops.embedding(table.cuda(), tokens.cuda(), 7.3)
+        oracle.assert_near(got, *oracle.embedding(table, tokens, float(torch.tensor(7.3))), f"{dtype} {wide}")
+
+
+def test_lookup_of_rows_apart_and_of_several_dimensions():
+    store = torch.randn(40, 136).bfloat16()
+    for first, width in ((0, 128), (8, 128), (3, 65)):
+        table = store[:, first:first + width]
+        tokens = tokens_of(30, 40, 2).reshape(5, 6)
+        got = ops.embedding(store.cuda()[:, first:first + width], tokens.cuda())
+        assert got.shape == (5, 6, width)
+        oracle.assert_near(got, *oracle.embedding(table, tokens, 1.0))
+
+
+def test_lookup_without_tokens_or_rows():
+    table = torch.randn(4, 16).cuda()
+    assert ops.embedding(table, torch.zeros(0, dtype=torch.int32, device="cuda")).shape == (0, 16)
+    got = ops.embedding(table[:0], torch.zeros(3, dtype=torch.int32, device="cuda"))
+    assert torch.equal(got, torch.zeros(3, 16, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,rows,width", [(1, 1, 1), (2, 3, 8), (31, 1, 40), (32, 1, 40), (33, 1, 40), (64, 2, 520), (1000, 300, 33), (2048, 255, 64), (2049, 257, 64),
+                                          (5000, 70000, 24), (4096, 65536, 16), (300, 17000000, 1)])
+def test_gradient(dtype, n, rows, width):
+    g = torch.Generator().manual_seed(n)
+    grad, tokens = torch.randn(n, width, generator=g).to(dtype), tokens_of(n, rows, n + 1)
+    scale = 0.75
+    if rows > 1000000:   # (three passes of the sort and more; compared where the tokens are)
+        out = ops.embedding_grad(grad.cuda(), tokens.cuda(), rows, scale)
+        ids, at = torch.unique(tokens[(tokens >= 0) & (tokens < rows)], return_inverse=True)
+        small = torch.full((n,), -1)
+        small[(tokens >= 0) & (tokens < rows)] = at
+        oracle.assert_near(out[ids.cuda()], *oracle.embedding_grad(grad, small, len(ids), scale, dtype))
+        assert int((out != 0).sum()) <= len(ids) * width
+        return
+    for out_dtype in {dtype, torch.float32}:
+        out = torch.full((rows, width), 77.0, dtype=out_dtype, device="cuda")
+        got = ops.embedding_grad(grad.cuda(), tokens.cuda(), rows, scale, out=out)
+        assert got is out
+        oracle.assert_near(got, *oracle.embedding_grad(grad, tokens, rows, scale, out_dtype), f"{dtype} {out_dtype}")
+    again = ops.embedding_grad(grad.cuda(), tokens.cuda().int(), rows, scale, out=torch.empty_like(out))
+    assert torch.equal(again, out)   # (int32 and int64 tokens, and from call to call)
+
+
+def test_gradient_adds_to_what_is_there():
+    grad, tokens = torch.randn(500, 72).bfloat16(), tokens_of(500, 90, 3)
+    old = torch.randn(90, 72)
+    out = old.cuda()
+    ops.embedding_grad(grad.cuda(), tokens.cuda(), 90, 2.0, out=out, accumulate=True)
+    oracle.assert_near(out, *oracle.embedding_grad(grad, tokens, 90, 2.0, torch.float32, old))
+    without = torch.ones(90, dtype=torch.bool)
+    without[tokens[(tokens >= 0) & (tokens < 90)]] = False
+    assert without.any() and torch.equal(out.cpu()[without], old[without])   # bit for bit
+    ops.embedding_grad(grad[:0].cuda(), tokens[:0].cuda(), 90, out=out, accumulate=True)
+
+
+def test_gradient_of_rows_apart_and_into_rows_apart():
+    store = torch.randn(100, 96).bfloat16()
+    tokens = tokens_of(100, 20, 4)
+    for first, width in ((0, 64), (8, 64), (1, 63)):
+        out = torch.full((20, 100), 3.0, device="cuda")
+        ops.embedding_grad(store.cuda()[:, first:first + width], tokens.cuda(), 20, out=out[:, 16:16 + width])
+        oracle.assert_near(out[:, 16:16 + width], *oracle.embedding_grad(store[:, first:first + width], tokens, 20, 1.0, torch.float32))
+        assert bool((out[:, :16] == 3).all()) and bool((out[:, 16 + width:] == 3).all())
+
+
+def test_gradient_without_tokens():
+    out = torch.full((10, 24), 5.0, device="cuda")
+    ops.embedding_grad(torch.zeros(0, 24, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"), 10, out=out)
+    assert bool((out == 0).all())
+    padded = ops.embedding_grad(torch.ones(70, 24, device="cuda"), torch.full((70,), -1, device="cuda"), 10)
+    assert bool((padded == 0).all())
+
+
+def test_gradient_keeps_infinities_and_nan_to_their_rows():
+    grad = torch.ones(40, 16)
+    grad[3, 5], grad[4, 6] = float("inf"), float("nan")
+    tokens = torch.arange(40) % 8
+    got = ops.embedding_grad(grad.cuda(), tokens.cuda(), 9).cpu()
+    assert got[3, 5] == float("inf") and torch.isnan(got[4, 6])
+    got[3, 5] = got[4, 6] = 5.0
+    assert torch.equal(got[:8], torch.full((8, 16), 5.0)) and torch.equal(got[8], torch.zeros(16))
+
+
+def test_lookup_and_gradient_of_a_table_of_more_than_4_gib():
+    # (rows whose place in the table does not fit 32 bits)
+    rows, width = 1100000, 2048
+    table = torch.zeros(rows, width, dtype=torch.bfloat16, device="cuda")
+    tokens = torch.tensor([rows - 1, 5, rows - 2, 0, rows - 1])
+    table[tokens.cuda()] = torch.randn(5, width, device="cuda").bfloat16()
+    got = ops.embedding(table, tokens.cuda())
+    assert torch.equal(got, table[tokens.cuda()])
+    grad = torch.randn(5, width, device="cuda").bfloat16()
+    back = ops.embedding_grad(grad, tokens.cuda(), rows, out=table)
+    ids, at = torch.unique(tokens, return_inverse=True)
+    oracle.assert_near(back[ids.cuda()], *oracle.embedding_grad(grad.cpu(), at, len(ids), 1.0, torch.bfloat16))
+    assert int((back != 0).any(1).sum()) == 4
