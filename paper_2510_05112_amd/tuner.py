@@ -311,6 +311,55 @@ def tune_shared(gen_handle, sync_handle, problem, shared_problem, k: int = 8, in
     return [dict(label=labels[int(i)], makespan=int(t), index=int(i), slid=False) for i, t in zip(idx, ms)]
 
 
+def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_backward: bool = True, repeats: int = 5):
+    """The cost table of a model's stages on this GPU, as the paper's profiler (Section 3) delivers it: every stage's F, B and W
+    items (``stages.Stage``) are run in turn on one micro-batch and timed.  tokens: [batch][steps] int32 or int64, the first
+    stage's input; targets: the last stage's, default tokens.  Returns dict(dur: int32 [8][S] in units of unit_us microseconds, at least
+    1 each, for ``Problem``: R and FD cost what F does, B is the whole backward pass without split_backward, O and L are 0;
+    us: float [8][S], the medians of the repeats; kept_bytes: int64 [S], what a stage holds of a micro-batch between its F and
+    its last backward item, for mem_units).  The weights' gradients are as before afterwards."""
+    import torch
+
+    from .stages import kept_bytes
+
+    if not stages or repeats < 1 or unit_us <= 0:
+        raise ValueError("measure_costs: stages, a positive unit and at least one repeat are needed")
+    targets = tokens if targets is None else targets
+    device = tokens.device
+    us, held = np.zeros((8, len(stages))), np.zeros(len(stages), np.int64)
+    inputs = tokens
+    with torch.cuda.device(device):
+        saved = [{name: g.clone() for name, g in layer.grads.items()} for stage in stages for layer in stage.layers if hasattr(layer, "grads")]
+        for s, stage in enumerate(stages):
+            times = []
+            for _ in range(repeats + 1):   # (the first: memory is allocated, code is loaded)
+                at = [torch.cuda.Event(enable_timing=True) for _ in range(4)]
+                at[0].record()
+                out, kept = stage.forward(inputs, targets)
+                at[1].record()
+                grad = 1.0 if out.dim() == 0 else torch.ones_like(out)
+                held[s] = kept_bytes(kept)
+                at_b = torch.cuda.Event(enable_timing=True)
+                at_b.record()
+                _, grad_kept = stage.input_grad(grad, kept)
+                at[2].record()
+                stage.weight_grad(kept, grad_kept)
+                at[3].record()
+                at[3].synchronize()
+                times.append((at[0].elapsed_time(at[1]), at_b.elapsed_time(at[2]), at[2].elapsed_time(at[3])))
+            us[1:4, s] = 1e3 * np.median(np.asarray(times[1:]), axis=0)
+            inputs = out
+        for layer, grads in zip([x for stage in stages for x in stage.layers if hasattr(x, "grads")], saved):
+            for name, g in grads.items():
+                layer.grads[name].copy_(g)
+    if not split_backward:
+        us[2] += us[3]
+        us[3] = 0
+    us[4] = us[7] = us[1]
+    dur = np.where(us > 0, np.maximum(1, np.rint(us / unit_us)), 0).astype(np.int32)
+    return dict(dur=dur, us=us, kept_bytes=held)
+
+
 def stride_for(problem) -> int:
     """Row stride (words, multiple of 8) that holds the longest list the generator can emit."""
     per_dev = int(np.bincount(np.asarray(problem.stage_device), minlength=int(problem.n_devices)).max())
