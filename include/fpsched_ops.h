@@ -65,7 +65,7 @@ int fpsched_op_embedding_grad(int device_id, int type, const void *grad, int64_t
  * kept (NULL, or float [n_batch][ceil(n_steps / FPSCHED_RECURRENCE_BLOCK)][width]): the state in front
  * of every block of steps, from which the backward pass starts.  One step (n_steps = 1) is the form for
  * serving.  n_batch < 2^16, width <= 2^24. */
-#define FPSCHED_RECURRENCE_BLOCK 128
+#define FPSCHED_RECURRENCE_BLOCK 64
 size_t fpsched_op_recurrence_workspace_bytes(int64_t n_batch, int64_t n_steps, int64_t width);
 int fpsched_op_recurrence(int device_id, int type, int64_t n_batch, int64_t n_steps, int64_t width,
                           const void *gate, const void *value, const int64_t *strides /* HOST [6] */,

@@ -1,24 +1,27 @@
 // Gated linear recurrence:  h[t] = a[t] h[t-1] + (1 - a[t]) v[t],  a = sigmoid(gate), for each sequence and channel.
 //
 // A step is an affine map of the state, and maps compose: of a run of steps (A, S) with h_end = A h_begin + S, two runs one after the other
-// have (A2 A1, A2 S1 + S2).  A workgroup walks a sequence in blocks of kWaves x kSteps = 128 steps for 64 lanes' channels (two adjacent ones a lane
-// where strides allow): each wavefront loads kSteps of them, works out its run's map from registers, the maps go round through LDS, and
-// each wavefront then takes its steps from the state that those in front of it leave.  Everything is read once and written once, the next block's
-// loads under way meanwhile.
+// have (A2 A1, A2 S1 + S2).  A workgroup walks a sequence in blocks of 64 steps for 64 lanes' channels (two adjacent ones a lane
+// where strides allow): each wavefront loads a run of 16 steps (8 in the backward pass), works out its map, the maps go round through LDS, and
+// each wavefront then takes its steps from the state that those in front of it leave.
 //
 // Few sequences of few channels leave most of the chip idle that way; they are cut into segments, whose maps
-// a first kernel works out (it reads gate and value once more), and each segment's workgroup begins by composing those in front of it.
+// a first kernel works out, and each segment's workgroup begins by composing those in front of it.
 //
 // The backward pass is the same walk from the end, of e[t-1] = a[t] (grad[t] + e[t]), where e is the gradient of the state from
 // what follows.  It needs h[t-1] to 32 bits: the forward pass leaves the state in front of every block
-// of 128 steps (at most 1/32 of what it reads), and the wavefronts work out the rest again from gate and value, which the backward pass reads anyway.
+// of 64 steps (at most 1/16 of what it reads), and the wavefronts work out the rest again from gate and value, which the backward pass reads anyway.
 #include "ops_common.h"
+
+#include <algorithm>
 
 namespace fpsched {
 namespace {
 
-constexpr int kWaves = 8, kSteps = 16, kBlock = FPSCHED_RECURRENCE_BLOCK;
-static_assert(kWaves * kSteps == kBlock, "a workgroup's steps are a block");
+constexpr int kBlock = FPSCHED_RECURRENCE_BLOCK;
+constexpr int kSteps = 16, kWaves = kBlock / kSteps;            // of a wavefront and of a workgroup, forward
+constexpr int kGradSteps = 8, kGradWaves = kBlock / kGradSteps;   // backward, which holds more of each step
+constexpr int kFewSteps = 8;
 
 // a = sigmoid(gate) and 1 - a.  The smaller one is worked out (a gate of 20 has 1 - a = 2e-9) and the other one rounded once from
 // it: a state is multiplied by a as many times as it has steps, and an error of the reciprocal in a would add up.
@@ -38,61 +41,64 @@ struct RecurrenceArgs {
   const T *gate, *value, *grad;
   T *out, *d_gate, *d_value;
   Strides s_gate, s_value, s_grad, s_out, s_d_gate, s_d_value;
-  const float *state;      // of the forward pass: in front of the first step; of the backward pass: the gradient behind the last
-  float *final_state;      // ... behind the last; the gradient in front of the first
+  const float *state;      // where the walk begins: in front of the first step; backward, the gradient behind the last
+  float *final_state;      // where it ends
   float *kept;             // [batch][blocks][width]
   const int32_t* lengths;
   float* segment_maps;     // [batch][segment][2][width]
   float* state_copy;       // [batch][width]
   int64_t steps, width;
-  int blocks, segment_blocks, segments;
+  int blocks, segment_blocks;   // of a sequence, of a segment
 };
 
-// One block of steps of a lane's channels in registers, steps [first, first + kSteps) of this wavefront.
-template <typename T, int N>
-__device__ __forceinline__ void load_steps(Vec<T, N> (&to)[kSteps], const T* from, int64_t step_stride, int64_t first, int64_t end) {
+__device__ __forceinline__ int64_t end_of(const int32_t* lengths, int64_t b, int64_t steps) {
+  return lengths ? min(max((int64_t)lengths[b], (int64_t)0), steps) : steps;
+}
+
+// Rows first ... of a tensor, a lane's channels from c on; of those from `end` on the last one in front of it (what is loaded is not used).
+// Rows are the same for all lanes.
+template <typename T, int N, int STEPS>
+__device__ __forceinline__ void load_steps(Vec<T, N> (&to)[STEPS], const T* from, int64_t step_stride, int64_t first, int64_t end, unsigned c) {
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    to[i] = {};
-    if (first + i < end) to[i] = load_vec<T, N>(from + (first + i) * step_stride);
-  }
+  for (int i = 0; i < STEPS; ++i) to[i] = load_vec<T, N>(from + max(min(first + i, end - 1), (int64_t)0) * step_stride + c);
 }
 
 enum { kForward, kBackward };
 
-// The maps of segments: forward (A, S) of its steps in order, backward (A, E) of them from the end.
+// The maps of segments: forward (A, S) of its steps in order, backward (A, E) of them from the end.  Of the walk's segments but the last.
 template <typename T, int N, int DIR>
 __global__ __launch_bounds__(kWaves * 64) void segment_maps_kernel(RecurrenceArgs<T> args) {
-  __shared__ float maps[kWaves][2][64 * N];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t b = blockIdx.y, segment = DIR == kForward ? blockIdx.z : blockIdx.z + 1;   // (nothing follows the walk's last)
-  const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * N;
-  const bool live = c < args.width;
-  const int64_t cc = live ? c : 0;
-  if (blockIdx.z == 0 && wave == 0 && live) {   // (the caller may have the walk's result where its start is: other segments' workgroups read a copy)
+  __shared__ Vec<float, 2 * N> maps[2][kWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t b = blockIdx.y;
+  const int turn = blockIdx.z;   // segments in the order of the walk
+  const int segments = gridDim.z + 1;
+  const unsigned at = (blockIdx.x * 64 + lane) * N;
+  const bool live = at < args.width;
+  const unsigned c = live ? at : 0;
+  if (turn == 0 && wave == 0 && live) {   // (the caller may have the walk's result where its start is: other segments' workgroups read a copy)
 #pragma unroll
     for (int k = 0; k < N; ++k) args.state_copy[b * args.width + c + k] = args.state ? args.state[b * args.width + c + k] : 0.f;
   }
-  const int64_t end = args.lengths ? min(max((int64_t)args.lengths[b], (int64_t)0), args.steps) : args.steps;
-  const T* gate = args.gate + b * args.s_gate.batch + cc;
-  const T* other = DIR == kForward ? args.value + b * args.s_value.batch + cc : args.grad + b * args.s_grad.batch + cc;
+  const int64_t end = end_of(args.lengths, b, args.steps);
+  const T* gate = args.gate + b * args.s_gate.batch;
+  const T* other = DIR == kForward ? args.value + b * args.s_value.batch : args.grad + b * args.s_grad.batch;
   const int64_t other_step = DIR == kForward ? args.s_value.step : args.s_grad.step;
+  const int segment = DIR == kForward ? turn : segments - 1 - turn;
+  const int first_block = segment * args.segment_blocks, last_block = min(first_block + args.segment_blocks, args.blocks);
   float A[N], S[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) A[k] = 1.f, S[k] = 0.f;
-  const int64_t first_block = segment * args.segment_blocks, last_block = min(first_block + args.segment_blocks, (int64_t)args.blocks);
-  // (each wavefront its share of the segment's blocks' steps, block by block: the maps of a wavefront's runs in different blocks are not
-  // adjacent, so they are composed block by block)
-  for (int64_t j = 0; j < last_block - first_block; ++j) {
-    const int64_t block = DIR == kForward ? first_block + j : last_block - 1 - j;
-    if (block * kBlock >= end) continue;
-    const int64_t first = block * kBlock + wave * kSteps;
+  for (int j = 0; j < last_block - first_block; ++j) {
+    // (the walk itself begins where this one ends, with what is still in cache)
+    const int block = DIR == kForward ? last_block - 1 - j : first_block + j;
+    const int64_t first = (int64_t)block * kBlock + wave * kSteps;
     Vec<T, N> g[kSteps], v[kSteps];
-    load_steps<T, N>(g, gate, args.s_gate.step, first, end);
-    load_steps<T, N>(v, other, other_step, first, end);
-    float a1[N], s1[N];
+    load_steps<T, N, kSteps>(g, gate, args.s_gate.step, first, end, c);
+    load_steps<T, N, kSteps>(v, other, other_step, first, end, c);
+    Vec<float, 2 * N> m;
 #pragma unroll
-    for (int k = 0; k < N; ++k) a1[k] = 1.f, s1[k] = 0.f;
+    for (int k = 0; k < N; ++k) m.at[k] = 1.f, m.at[N + k] = 0.f;
 #pragma unroll
     for (int n = 0; n < kSteps; ++n) {
       const int i = DIR == kForward ? n : kSteps - 1 - n;
@@ -101,194 +107,259 @@ __global__ __launch_bounds__(kWaves * 64) void segment_maps_kernel(RecurrenceArg
         for (int k = 0; k < N; ++k) {
           float a, na;
           gates((float)g[i].at[k], &a, &na);
-          if (DIR == kForward) s1[k] = a * s1[k] + na * (float)v[i].at[k];
-          else s1[k] = a * (s1[k] + (float)v[i].at[k]);
-          a1[k] *= a;
+          if (DIR == kForward) m.at[N + k] = a * m.at[N + k] + na * (float)v[i].at[k];
+          else m.at[N + k] = a * (m.at[N + k] + (float)v[i].at[k]);
+          m.at[k] *= a;
         }
       }
     }
+    maps[j & 1][wave][lane] = m;
+    __syncthreads();   // (the next block's maps go to the other half)
 #pragma unroll
-    for (int k = 0; k < N; ++k) maps[wave][0][lane * N + k] = a1[k], maps[wave][1][lane * N + k] = s1[k];
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < kWaves; ++n) {
-      const int w = DIR == kForward ? n : kWaves - 1 - n;
+    for (int n = 0; n < kWaves; ++n) {   // (in front of what is composed already)
+      const Vec<float, 2 * N> o = maps[j & 1][DIR == kForward ? kWaves - 1 - n : n][lane];
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        const float a2 = maps[w][0][lane * N + k];
-        S[k] = a2 * S[k] + maps[w][1][lane * N + k];
-        A[k] *= a2;
+        S[k] += A[k] * o.at[N + k];
+        A[k] *= o.at[k];
       }
     }
-    __syncthreads();
   }
   if (live && wave == 0) {
-    float* to = args.segment_maps + ((b * args.segments + segment) * 2) * args.width + c;
+    float* to = args.segment_maps + (b * segments + turn) * 2 * args.width + c;
 #pragma unroll
     for (int k = 0; k < N; ++k) to[k] = A[k], to[args.width + k] = S[k];
   }
 }
 
-template <typename T, int N, bool KEEP>
-__global__ __launch_bounds__(kWaves * 64) void recurrence_kernel(RecurrenceArgs<T> args) {
-  __shared__ float maps[2][kWaves][2][64 * N];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t b = blockIdx.y, segment = blockIdx.z;
-  const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * N;
-  const bool live = c < args.width;
-  const int64_t cc = live ? c : 0;
-  const int64_t end = args.lengths ? min(max((int64_t)args.lengths[b], (int64_t)0), args.steps) : args.steps;
-  const T* gate = args.gate + b * args.s_gate.batch + cc;
-  const T* value = args.value + b * args.s_value.batch + cc;
-  T* out = args.out + b * args.s_out.batch + cc;
-  float h[N];   // the state in front of the block
+// A lane's channels of the walk's state in front of its turn-th segment.
+template <typename T, int N>
+__device__ __forceinline__ void begin_walk(const RecurrenceArgs<T>& args, int64_t b, int turn, int segments, unsigned c, float (&h)[N]) {
 #pragma unroll
-  for (int k = 0; k < N; ++k) h[k] = args.state ? args.state[b * args.width + cc + k] : 0.f;
-  for (int64_t s = 0; s < segment; ++s) {
-    const float* m = args.segment_maps + ((b * args.segments + s) * 2) * args.width + cc;
+  for (int k = 0; k < N; ++k) h[k] = args.state ? args.state[b * args.width + c + k] : 0.f;
+  const float* m = args.segment_maps + b * segments * 2 * args.width + c;
+  for (int s = 0; s < turn; ++s, m += 2 * args.width) {
 #pragma unroll
     for (int k = 0; k < N; ++k) h[k] = m[k] * h[k] + m[args.width + k];
   }
-  const int64_t first_block = segment * args.segment_blocks, last_block = min(first_block + args.segment_blocks, (int64_t)args.blocks);
-  Vec<T, N> g[kSteps], v[kSteps];
-  load_steps<T, N>(g, gate, args.s_gate.step, first_block * kBlock + wave * kSteps, end);
-  load_steps<T, N>(v, value, args.s_value.step, first_block * kBlock + wave * kSteps, end);
-  for (int64_t block = first_block; block < last_block; ++block) {
-    if (KEEP && live && wave == 0) {
-      float* to = args.kept + (b * args.blocks + block) * args.width + c;
+}
+
+template <typename T, int N, bool KEEP>
+__global__ __launch_bounds__(kWaves * 64, 4) void recurrence_kernel(RecurrenceArgs<T> args) {
+  __shared__ Vec<float, 2 * N> maps[2][kWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t b = blockIdx.y;
+  const int segment = blockIdx.z, segments = gridDim.z;
+  const unsigned at = (blockIdx.x * 64 + lane) * N;
+  const bool live = at < args.width;
+  const unsigned c = live ? at : 0;
+  const int64_t end = end_of(args.lengths, b, args.steps);
+  const T *gate = args.gate + b * args.s_gate.batch, *value = args.value + b * args.s_value.batch;
+  T* out = args.out + b * args.s_out.batch;
+  float h[N];   // the state in front of the block
+  begin_walk<T, N>(args, b, segment, segments, c, h);
+  const int first_block = segment * args.segment_blocks, last_block = min(first_block + args.segment_blocks, args.blocks);
+  for (int block = first_block; block < last_block; ++block) {
+    const int64_t first = (int64_t)block * kBlock + wave * kSteps;
+    float a[kSteps][N], s[kSteps][N];
+    {
+      Vec<T, N> g[kSteps], v[kSteps];
+      load_steps<T, N, kSteps>(g, gate, args.s_gate.step, first, end, c);
+      load_steps<T, N, kSteps>(v, value, args.s_value.step, first, end, c);
+      if (KEEP && live && wave == 0) {
+        float* to = args.kept + (b * args.blocks + block) * args.width + c;
 #pragma unroll
-      for (int k = 0; k < N; ++k) to[k] = h[k];
+        for (int k = 0; k < N; ++k) to[k] = h[k];
+      }
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          float na;
+          gates((float)g[i].at[k], &a[i][k], &na);
+          s[i][k] = na * (float)v[i].at[k];
+        }
+      }
     }
-    const int64_t first = block * kBlock + wave * kSteps;
-    float a[kSteps][N], s[kSteps][N], A[N], S[N];
+    if (first + kSteps > end) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) A[k] = 1.f, S[k] = 0.f;
+      for (int i = 0; i < kSteps; ++i)
+        if (first + i >= end) {
+#pragma unroll
+          for (int k = 0; k < N; ++k) a[i][k] = 1.f, s[i][k] = 0.f;
+        }
+    }
+    Vec<float, 2 * N> m;
+#pragma unroll
+    for (int k = 0; k < N; ++k) m.at[k] = 1.f, m.at[N + k] = 0.f;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        float na;
-        gates((float)g[i].at[k], &a[i][k], &na);
-        s[i][k] = na * (float)v[i].at[k];
-        if (first + i >= end) a[i][k] = 1.f, s[i][k] = 0.f;
-        S[k] = a[i][k] * S[k] + s[i][k];
-        A[k] *= a[i][k];
+        m.at[N + k] = a[i][k] * m.at[N + k] + s[i][k];
+        m.at[k] *= a[i][k];
       }
     }
-    if (block + 1 < last_block) {
-      load_steps<T, N>(g, gate, args.s_gate.step, first + kBlock, end);
-      load_steps<T, N>(v, value, args.s_value.step, first + kBlock, end);
-    }
-    float(&m)[kWaves][2][64 * N] = maps[block & 1];
-#pragma unroll
-    for (int k = 0; k < N; ++k) m[wave][0][lane * N + k] = A[k], m[wave][1][lane * N + k] = S[k];
-    __syncthreads();   // (the other half of `maps` is the next block's: one barrier a block)
+    maps[block & 1][wave][lane] = m;
+    __syncthreads();   // (the next block's maps go to the other half: one barrier a block)
     float mine[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) mine[k] = h[k];
-#pragma unroll
     for (int w = 0; w < kWaves; ++w) {
+      const Vec<float, 2 * N> o = maps[block & 1][w][lane];
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         if (w == wave) mine[k] = h[k];
-        h[k] = m[w][0][lane * N + k] * h[k] + m[w][1][lane * N + k];
+        h[k] = o.at[k] * h[k] + o.at[N + k];
       }
     }
+    T* row = out + first * args.s_out.step;
+    if (first + kSteps <= end) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      if (first + i >= args.steps) break;
-      Vec<T, N> o;
+      for (int i = 0; i < kSteps; ++i, row += args.s_out.step) {
+        Vec<T, N> o;
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        mine[k] = a[i][k] * mine[k] + s[i][k];
-        o.at[k] = (T)(first + i < end ? mine[k] : 0.f);
+        for (int k = 0; k < N; ++k) {
+          mine[k] = a[i][k] * mine[k] + s[i][k];
+          o.at[k] = (T)mine[k];
+        }
+        if (live) store_vec<T, N>(row + c, o);
       }
-      if (live) store_vec<T, N>(out + (first + i) * args.s_out.step, o);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i, row += args.s_out.step) {
+        if (first + i >= args.steps) break;
+        Vec<T, N> o;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          mine[k] = a[i][k] * mine[k] + s[i][k];
+          o.at[k] = (T)(first + i < end ? mine[k] : 0.f);
+        }
+        if (live) store_vec<T, N>(row + c, o);
+      }
     }
   }
-  if (live && wave == 0 && segment == args.segments - 1) {
+  if (live && wave == 0 && segment == segments - 1) {
 #pragma unroll
     for (int k = 0; k < N; ++k) args.final_state[b * args.width + c + k] = h[k];
   }
 }
 
+// At most kFewSteps steps: a lane takes its channels from first to last.
 template <typename T, int N>
-__global__ __launch_bounds__(kWaves * 64) void recurrence_grad_kernel(RecurrenceArgs<T> args) {
-  __shared__ float maps[2][kWaves][4][64 * N];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t b = blockIdx.y, segment = blockIdx.z;
-  const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * N;
-  const bool live = c < args.width;
-  const int64_t cc = live ? c : 0;
-  const int64_t end = args.lengths ? min(max((int64_t)args.lengths[b], (int64_t)0), args.steps) : args.steps;
-  const T* gate = args.gate + b * args.s_gate.batch + cc;
-  const T* value = args.value + b * args.s_value.batch + cc;
-  const T* grad = args.grad + b * args.s_grad.batch + cc;
-  T* d_gate = args.d_gate + b * args.s_d_gate.batch + cc;
-  T* d_value = args.d_value + b * args.s_d_value.batch + cc;
-  float e[N];   // the gradient of the state behind the block
+__global__ __launch_bounds__(256) void few_steps_kernel(RecurrenceArgs<T> args) {
+  const int64_t b = blockIdx.y;
+  const unsigned c = (blockIdx.x * 256 + threadIdx.x) * N;
+  if (c >= args.width) return;
+  const int64_t end = end_of(args.lengths, b, args.steps);
+  const T *gate = args.gate + b * args.s_gate.batch, *value = args.value + b * args.s_value.batch;
+  T* out = args.out + b * args.s_out.batch;
+  Vec<float, N> h = {};
+  if (args.state) {
 #pragma unroll
-  for (int k = 0; k < N; ++k) e[k] = args.state ? args.state[b * args.width + cc + k] : 0.f;
-  for (int64_t s = args.segments - 1; s > segment; --s) {
-    const float* m = args.segment_maps + ((b * args.segments + s) * 2) * args.width + cc;
-#pragma unroll
-    for (int k = 0; k < N; ++k) e[k] = m[k] * e[k] + m[args.width + k];
+    for (int k = 0; k < N; ++k) h.at[k] = args.state[b * args.width + c + k];
   }
-  const int64_t first_block = segment * args.segment_blocks, last_block = min(first_block + args.segment_blocks, (int64_t)args.blocks);
-  Vec<T, N> g[kSteps], v[kSteps], d[kSteps];
-  auto load = [&](int64_t block) {
-    const int64_t first = block * kBlock + wave * kSteps;
-    load_steps<T, N>(g, gate, args.s_gate.step, first, end);
-    load_steps<T, N>(v, value, args.s_value.step, first, end);
-    load_steps<T, N>(d, grad, args.s_grad.step, first, end);
-  };
-  if (last_block > first_block) load(last_block - 1);
-  for (int64_t block = last_block - 1; block >= first_block; --block) {
-    const int64_t first = block * kBlock + wave * kSteps;
-    float h[N];
+  if (args.kept) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) h[k] = args.kept[(b * args.blocks + block) * args.width + cc + k];
-    float A[N], S[N], E[N];
-#pragma unroll
-    for (int k = 0; k < N; ++k) A[k] = 1.f, S[k] = 0.f, E[k] = 0.f;
-    float a[kSteps][N], na[kSteps][N];
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
+    for (int k = 0; k < N; ++k) args.kept[b * args.width + c + k] = h.at[k];
+  }
+  for (int64_t t = 0; t < args.steps; ++t) {
+    Vec<T, N> o = {};
+    if (t < end) {
+      const Vec<T, N> g = load_vec<T, N>(gate + t * args.s_gate.step + c), v = load_vec<T, N>(value + t * args.s_value.step + c);
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        gates((float)g[i].at[k], &a[i][k], &na[i][k]);
-        if (first + i >= end) a[i][k] = 1.f, na[i][k] = 0.f;   // (value and grad are zero there)
-        S[k] = a[i][k] * S[k] + na[i][k] * (float)v[i].at[k];
-        A[k] *= a[i][k];
+        float a, na;
+        gates((float)g.at[k], &a, &na);
+        h.at[k] = a * h.at[k] + na * (float)v.at[k];
+        o.at[k] = (T)h.at[k];
+      }
+    }
+    store_vec<T, N>(out + t * args.s_out.step + c, o);
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) args.final_state[b * args.width + c + k] = h.at[k];
+}
+
+template <typename T, int N>
+__global__ __launch_bounds__(kGradWaves * 64) void recurrence_grad_kernel(RecurrenceArgs<T> args) {
+  __shared__ Vec<float, 2 * N> maps[2][kGradWaves][64];
+  __shared__ Vec<float, N> map_grads[2][kGradWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t b = blockIdx.y;
+  const int segments = gridDim.z, segment = blockIdx.z;
+  const unsigned at = (blockIdx.x * 64 + lane) * N;
+  const bool live = at < args.width;
+  const unsigned c = live ? at : 0;
+  const int64_t end = end_of(args.lengths, b, args.steps);
+  const T *gate = args.gate + b * args.s_gate.batch, *value = args.value + b * args.s_value.batch, *grad = args.grad + b * args.s_grad.batch;
+  T *d_gate = args.d_gate + b * args.s_d_gate.batch, *d_value = args.d_value + b * args.s_d_value.batch;
+  float e[N];   // the gradient of the state behind the block
+  begin_walk<T, N>(args, b, segments - 1 - segment, segments, c, e);
+  const int first_block = segment * args.segment_blocks, last_block = min(first_block + args.segment_blocks, args.blocks);
+  for (int block = last_block - 1; block >= first_block; --block) {
+    const int64_t first = (int64_t)block * kBlock + wave * kGradSteps;
+    Vec<T, N> g[kGradSteps], v[kGradSteps], d[kGradSteps];
+    load_steps<T, N, kGradSteps>(g, gate, args.s_gate.step, first, end, c);
+    load_steps<T, N, kGradSteps>(v, value, args.s_value.step, first, end, c);
+    load_steps<T, N, kGradSteps>(d, grad, args.s_grad.step, first, end, c);
+    float h[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) h[k] = args.kept[(b * args.blocks + block) * args.width + c + k];
+    const bool whole = first + kGradSteps <= end;
+    float a[kGradSteps][N], na[kGradSteps][N];
+#pragma unroll
+    for (int i = 0; i < kGradSteps; ++i) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) gates((float)g[i].at[k], &a[i][k], &na[i][k]);
+    }
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < kGradSteps; ++i)
+        if (first + i >= end) {
+          v[i] = {}, d[i] = {};
+#pragma unroll
+          for (int k = 0; k < N; ++k) a[i][k] = 1.f, na[i][k] = 0.f;
+        }
+    }
+    Vec<float, 2 * N> m;
+    Vec<float, N> E = {};
+#pragma unroll
+    for (int k = 0; k < N; ++k) m.at[k] = 1.f, m.at[N + k] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kGradSteps; ++i) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        m.at[N + k] = a[i][k] * m.at[N + k] + na[i][k] * (float)v[i].at[k];
+        m.at[k] *= a[i][k];
       }
     }
 #pragma unroll
-    for (int i = kSteps - 1; i >= 0; --i) {
+    for (int i = kGradSteps - 1; i >= 0; --i) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) E[k] = a[i][k] * ((float)d[i].at[k] + E[k]);
+      for (int k = 0; k < N; ++k) E.at[k] = a[i][k] * ((float)d[i].at[k] + E.at[k]);
     }
-    float(&m)[kWaves][4][64 * N] = maps[block & 1];
-#pragma unroll
-    for (int k = 0; k < N; ++k) m[wave][0][lane * N + k] = A[k], m[wave][1][lane * N + k] = S[k], m[wave][2][lane * N + k] = E[k];
+    maps[block & 1][wave][lane] = m;
+    map_grads[block & 1][wave][lane] = E;
     __syncthreads();
     float behind[N];
+    for (int w = 0; w < wave; ++w) {
+      const Vec<float, 2 * N> o = maps[block & 1][w][lane];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      if (w >= wave) break;
-#pragma unroll
-      for (int k = 0; k < N; ++k) h[k] = m[w][0][lane * N + k] * h[k] + m[w][1][lane * N + k];
+      for (int k = 0; k < N; ++k) h[k] = o.at[k] * h[k] + o.at[N + k];
     }
 #pragma unroll
-    for (int w = kWaves - 1; w >= 0; --w) {
+    for (int w = kGradWaves - 1; w >= 0; --w) {
+      const Vec<float, 2 * N> o = maps[block & 1][w][lane];
+      const Vec<float, N> og = map_grads[block & 1][w][lane];
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         if (w == wave) behind[k] = e[k];
-        e[k] = m[w][0][lane * N + k] * e[k] + m[w][2][lane * N + k];
+        e[k] = o.at[k] * e[k] + og.at[k];
       }
     }
-    float before[kSteps][N];   // the state in front of each step, less its value
+    float before[kGradSteps][N];   // the state in front of each step, less its value
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
+    for (int i = 0; i < kGradSteps; ++i) {
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         const float x = (float)v[i].at[k];
@@ -297,22 +368,21 @@ __global__ __launch_bounds__(kWaves * 64) void recurrence_grad_kernel(Recurrence
       }
     }
 #pragma unroll
-    for (int i = kSteps - 1; i >= 0; --i) {
+    for (int i = kGradSteps - 1; i >= 0; --i) {
       Vec<T, N> dg, dv;
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         const float now = (float)d[i].at[k] + behind[k];
-        const bool in = first + i < end;
-        dv.at[k] = (T)(in ? na[i][k] * now : 0.f);
-        dg.at[k] = (T)(in ? now * before[i][k] * (a[i][k] * na[i][k]) : 0.f);
+        dv.at[k] = (T)(na[i][k] * now);
+        dg.at[k] = (T)(now * before[i][k] * (a[i][k] * na[i][k]));
         behind[k] = a[i][k] * now;
       }
+      if (!whole && first + i >= end) dg = {}, dv = {};   // (a state that is infinite makes 0 times it no number)
       if (live && first + i < args.steps) {
-        store_vec<T, N>(d_value + (first + i) * args.s_d_value.step, dv);
-        store_vec<T, N>(d_gate + (first + i) * args.s_d_gate.step, dg);
+        store_vec<T, N>(d_value + (first + i) * args.s_d_value.step + c, dv);
+        store_vec<T, N>(d_gate + (first + i) * args.s_d_gate.step + c, dg);
       }
     }
-    if (block > first_block) load(block - 1);
   }
   if (live && wave == 0 && segment == 0 && args.final_state) {
 #pragma unroll
@@ -320,8 +390,8 @@ __global__ __launch_bounds__(kWaves * 64) void recurrence_grad_kernel(Recurrence
   }
 }
 
-// Segments of a sequence: enough for two workgroups a compute unit, of four blocks at least (what a segment
-// costs is the second reading of its steps, and its turn in the composition that every later segment begins with).
+// Segments of a sequence: enough for four workgroups a compute unit, and none where there are two each without (a segment's steps are read
+// twice).
 struct Cut {
   int blocks, segment_blocks, segments;
 };
@@ -330,8 +400,8 @@ Cut cut(int64_t n_batch, int64_t n_steps, int64_t width) {
   Cut s;
   s.blocks = (int)ceil_div(n_steps, kBlock);
   const int64_t groups = std::max<int64_t>(1, n_batch * ceil_div(width, 128));
-  const int64_t wanted = std::min<int64_t>(ceil_div(512, groups), ceil_div(s.blocks, 4));
-  s.segment_blocks = (int)std::max<int64_t>(1, ceil_div(s.blocks, std::max<int64_t>(1, wanted)));
+  s.segment_blocks = std::max(s.blocks, 1);
+  if (groups < 512 && s.blocks > 1) s.segment_blocks = (int)ceil_div(s.blocks, std::min<int64_t>(ceil_div(1024, groups), s.blocks));
   s.segments = (int)std::max<int64_t>(1, ceil_div(s.blocks, s.segment_blocks));
   return s;
 }
@@ -340,6 +410,20 @@ constexpr int64_t kMostStride = 1ll << 31;   // (times a count of steps far from
 
 bool sizes_fit(int64_t n_batch, int64_t n_steps, int64_t width) {
   return n_batch >= 0 && n_batch <= 65535 && n_steps >= 0 && n_steps <= 0x7fffffffll && width >= 0 && width <= (1 << 24);
+}
+
+// Both kernels, maps(args, grid) and then walk(args, grid), or the walk alone.
+template <typename T, typename M, typename W>
+void run_walk(RecurrenceArgs<T> a, const Cut& s, int64_t n_batch, unsigned x, float* workspace, M maps, W walk) {
+  a.blocks = s.blocks;
+  a.segment_blocks = s.segment_blocks;
+  if (s.segments > 1) {
+    a.segment_maps = workspace;
+    a.state_copy = workspace + n_batch * s.segments * 2 * a.width;
+    maps(a, dim3(x, (unsigned)n_batch, s.segments - 1));
+    a.state = a.state_copy;
+  }
+  walk(a, dim3(x, (unsigned)n_batch, s.segments));
 }
 
 // Whether no two elements of an output share memory: the steps of a sequence behind one another, or the sequences of a step.
@@ -394,19 +478,20 @@ int fpsched_op_recurrence(int device_id, int type, int64_t n_batch, int64_t n_st
     a.gate = static_cast<const T*>(gate); a.value = static_cast<const T*>(value); a.out = static_cast<T*>(out);
     a.s_gate = {strides[0], strides[1]}; a.s_value = {strides[2], strides[3]}; a.s_out = {strides[4], strides[5]};
     a.state = state; a.final_state = final_state; a.kept = kept; a.lengths = lengths;
-    a.segment_maps = static_cast<float*>(d_workspace);
-    a.state_copy = a.segment_maps + n_batch * s.segments * 2 * width;
-    a.steps = n_steps; a.width = width; a.blocks = s.blocks; a.segment_blocks = s.segment_blocks; a.segments = s.segments;
+    a.steps = n_steps; a.width = width;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return with_channels<T>(width, {gate, value, out}, {strides[0], strides[1], strides[2], strides[3], strides[4], strides[5]}, [&](auto n) {
       constexpr int N = decltype(n)::value;
-      const unsigned x = (unsigned)ceil_div(width, 64 * N);
-      if (s.segments > 1) {
-        segment_maps_kernel<T, N, kForward><<<dim3(x, (unsigned)n_batch, s.segments - 1), dim3(kWaves * 64), 0, stream>>>(a);
-        a.state = a.state_copy;
+      if (n_steps <= kFewSteps) {
+        few_steps_kernel<T, N><<<dim3((unsigned)ceil_div(width, 256 * N), (unsigned)n_batch), dim3(256), 0, stream>>>(a);
+        return launched();
       }
-      if (kept) recurrence_kernel<T, N, true><<<dim3(x, (unsigned)n_batch, s.segments), dim3(kWaves * 64), 0, stream>>>(a);
-      else recurrence_kernel<T, N, false><<<dim3(x, (unsigned)n_batch, s.segments), dim3(kWaves * 64), 0, stream>>>(a);
+      run_walk(a, s, n_batch, (unsigned)ceil_div(width, 64 * N), static_cast<float*>(d_workspace),
+                  [&](const RecurrenceArgs<T>& m, dim3 grid) { segment_maps_kernel<T, N, kForward><<<grid, dim3(kWaves * 64), 0, stream>>>(m); },
+                  [&](const RecurrenceArgs<T>& w, dim3 grid) {
+                    if (kept) recurrence_kernel<T, N, true><<<grid, dim3(kWaves * 64), 0, stream>>>(w);
+                    else recurrence_kernel<T, N, false><<<grid, dim3(kWaves * 64), 0, stream>>>(w);
+                  });
       return launched();
     });
   });
@@ -439,20 +524,15 @@ int fpsched_op_recurrence_grad(int device_id, int type, int64_t n_batch, int64_t
     a.s_grad = {strides[0], strides[1]}; a.s_gate = {strides[2], strides[3]}; a.s_value = {strides[4], strides[5]};
     a.s_d_gate = {strides[6], strides[7]}; a.s_d_value = {strides[8], strides[9]};
     a.state = grad_state; a.final_state = d_state; a.kept = const_cast<float*>(kept); a.lengths = lengths;
-    a.segment_maps = static_cast<float*>(d_workspace);
-    a.state_copy = a.segment_maps + n_batch * s.segments * 2 * width;
-    a.steps = n_steps; a.width = width; a.blocks = s.blocks; a.segment_blocks = s.segment_blocks; a.segments = s.segments;
+    a.steps = n_steps; a.width = width;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return with_channels<T>(width, {grad, gate, value, d_gate, d_value},
                             {strides[0], strides[1], strides[2], strides[3], strides[4], strides[5], strides[6], strides[7], strides[8], strides[9]},
                             [&](auto n) {
       constexpr int N = decltype(n)::value;
-      const unsigned x = (unsigned)ceil_div(width, 64 * N);
-      if (s.segments > 1) {
-        segment_maps_kernel<T, N, kBackward><<<dim3(x, (unsigned)n_batch, s.segments - 1), dim3(kWaves * 64), 0, stream>>>(a);
-        a.state = a.state_copy;
-      }
-      recurrence_grad_kernel<T, N><<<dim3(x, (unsigned)n_batch, s.segments), dim3(kWaves * 64), 0, stream>>>(a);
+      run_walk(a, s, n_batch, (unsigned)ceil_div(width, 64 * N), static_cast<float*>(d_workspace),
+                  [&](const RecurrenceArgs<T>& m, dim3 grid) { segment_maps_kernel<T, N, kBackward><<<grid, dim3(kWaves * 64), 0, stream>>>(m); },
+                  [&](const RecurrenceArgs<T>& w, dim3 grid) { recurrence_grad_kernel<T, N><<<grid, dim3(kGradWaves * 64), 0, stream>>>(w); });
       return launched();
     });
   });

@@ -19,7 +19,7 @@ import ctypes
 
 from .binding import FpschedError, load_library
 
-BLOCK = 128   # steps between the states that ``gated_recurrence`` keeps (FPSCHED_RECURRENCE_BLOCK)
+BLOCK = 64   # steps between the states that ``gated_recurrence`` keeps (FPSCHED_RECURRENCE_BLOCK)
 MAX_ALTERNATIVES = 32
 _ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 
