@@ -6,8 +6,10 @@
 // bytes of logits at a time and changes its m only where one of them is larger.  Rows are cut into parts where there are fewer rows than
 // the chip has room for; a second kernel puts the parts together.
 //
-// Alternatives: a wavefront keeps its logits of the part in registers, every lane names its best, and k times the best of
-// those is taken and its lane names the next one (logits are compared as integers in their order, with the id behind, so that equal ones come by ascending id).
+// Alternatives: the lanes keep their logits of the part in registers.  The k-th largest of a wavefront's lanes' largest logits has k logits at
+// least that are not below it; those of the whole part that are not below the highest of the wavefronts' such bars are
+// collected in LDS (about k of them), and each finds its place by counting the larger ones.  Equal logits come by ascending id: a candidate is
+// the logit's bits, in an order in which they compare as integers, with the id behind.  Where too many are equal to the bar (a row of one value) the k are found one by one.
 //
 // Masked logits are minus infinity, and x - m = -infinity gives e = 0, but 0 times it is NaN: factors are held at -1000.  m begins at the
 // type's lowest number and not at minus infinity, so that a row of masks needs no branch: its s stays 0.
@@ -83,6 +85,20 @@ __device__ __forceinline__ unsigned long long wave_most(unsigned long long a) {
   return a;
 }
 
+constexpr int kRoom = 512;   // candidates in LDS
+
+// The k largest of n distinct candidates in LDS, by one wavefront: put(place, candidate) for those places that there are.
+template <typename P>
+__device__ __forceinline__ void by_rank(const unsigned long long* candidates, int n, int k, int lane, P put) {
+  for (int first = 0; first < n; first += 64) {
+    const unsigned long long mine = first + lane < n ? candidates[first + lane] : 0;
+    int larger = 0;
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) larger += candidates[i] > mine;
+    if (mine && larger < k) put(larger, mine);
+  }
+}
+
 struct PartOut {          // [row][part]
   Stats* stats;
   unsigned long long* best;   // [row][part][k], descending
@@ -128,7 +144,9 @@ template <typename T, bool ALT>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
   constexpr int N = kWide<T>;
   __shared__ Stats wave_sums[kWaves];
-  __shared__ unsigned long long wave_best[kWaves][kMostAlternatives];
+  __shared__ unsigned long long candidates[ALT ? kRoom : 1];
+  __shared__ float bars[kWaves];
+  __shared__ int collected;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = row_out.k;
   const int64_t row = blockIdx.x / part_out.parts, part = blockIdx.x % part_out.parts;
   const T* logits = row_out.logits + row * row_out.stride;
@@ -175,59 +193,81 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, P
       for (int i = 0; i < kAhead; ++i) take(v[i]);
     }
   }
+  float bar = -INFINITY;
+  if constexpr (ALT) {
+    // the lane's largest, and how many lanes' are larger (or as large, of lanes in front)
+    float most = -INFINITY;
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+      for (int i = 0; i < N; ++i) most = fmaxf(most, (float)held[p].at[i]);
+    int larger = 0;
+#pragma unroll
+    for (int l = 0; l < 64; ++l) {
+      const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(most), l));
+      larger += other > most || (other == most && l < lane);
+    }
+    const unsigned long long at = __ballot(larger == k - 1);
+    bar = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(most), __builtin_ctzll(at)));
+    if (lane == 0) bars[wave] = bar;
+    if (threadIdx.x == 0) collected = 0;
+  }
   const Stats sums = wave_stats(mine);
   if (lane == 0) wave_sums[wave] = sums;
+  __syncthreads();
   if constexpr (ALT) {
-    // the lane's best below `bar`
-    auto next = [&](unsigned long long bar) {
-      unsigned long long best = 0;
 #pragma unroll
-      for (int p = 0; p < kPieces; ++p) {
-        const int64_t at = first + (int64_t)p * kThreads * N;
+    for (int w = 0; w < kWaves; ++w) bar = fmaxf(bar, bars[w]);
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      float most = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < N; ++i) most = fmaxf(most, (float)held[p].at[i]);
+      if (most >= bar && most > -INFINITY) {
+        const int64_t id = first + (int64_t)p * kThreads * N;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const unsigned long long r = at + i >= begin && at + i < end ? ranked(logit(held[p].at[i]), (unsigned)(at + i)) : 0;
-          if (r < bar && r > best) best = r;
+          const float x = logit(held[p].at[i]);
+          if (x >= bar && x > -INFINITY) {   // (what is outside the part is held as minus infinity)
+            const int place = atomicAdd(&collected, 1);   // (in any order: places among them are found by value)
+            if (place < kRoom) candidates[place] = ranked(x, (unsigned)(id + i));
+          }
         }
       }
-      return best;
-    };
-    unsigned long long best = next(~0ull);
-    for (int i = 0; i < k; ++i) {
-      const unsigned long long most = wave_most(best);
-      if (lane == 0) wave_best[wave][i] = most;
-      if (best == most && most) best = next(most);
     }
+    __syncthreads();
   }
-  __syncthreads();
-  if (wave) return;
-  Stats all = wave_sums[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) all.join(wave_sums[w]);
   const bool whole = part_out.parts == 1;
   const int64_t at = row * part_out.parts + part;
-  if (lane == 0) {
-    if (whole) row_out.put(row, all);
-    else part_out.stats[at] = all;
-  }
-  if constexpr (ALT) {
-    unsigned long long mine_of[kWaves * kMostAlternatives / 64];
+  if (wave == 0) {
+    Stats all = wave_sums[0];
 #pragma unroll
-    for (int j = 0; j < kWaves * kMostAlternatives / 64; ++j) {
-      const int n = j * 64 + lane;
-      mine_of[j] = n < kWaves * k ? wave_best[n / k][n % k] : 0;
+    for (int w = 1; w < kWaves; ++w) all.join(wave_sums[w]);
+    if (lane == 0) {
+      if (whole) row_out.put(row, all);
+      else part_out.stats[at] = all;
     }
-    for (int i = 0; i < k; ++i) {
-      unsigned long long best = 0;
-#pragma unroll
-      for (int j = 0; j < kWaves * kMostAlternatives / 64; ++j) best = mine_of[j] > best ? mine_of[j] : best;
-      best = wave_most(best);
-#pragma unroll
-      for (int j = 0; j < kWaves * kMostAlternatives / 64; ++j)
-        if (mine_of[j] == best) mine_of[j] = 0;
-      if (lane == 0) {
-        if (whole) row_out.put_alternative(row, i, best, all);
-        else part_out.best[at * k + i] = best;
+    if constexpr (ALT) {
+      const int n = collected;
+      auto put = [&](int i, unsigned long long r) {
+        if (whole) row_out.put_alternative(row, i, r, all);
+        else part_out.best[at * k + i] = r;
+      };
+      if (n <= kRoom) {
+        by_rank(candidates, n, k, lane, put);
+        if (lane >= n && lane < k) put(lane, 0);
+      } else {
+        unsigned long long below = ~0ull;
+        for (int i = 0; i < k; ++i) {
+          unsigned long long best = 0;
+          for (int64_t id = begin + lane; id < end; id += 64) {
+            const float x = logit(logits[id]);
+            const unsigned long long r = ranked(x, (unsigned)id);
+            if (x > -INFINITY && r < below && r > best) best = r;
+          }
+          below = wave_most(best);
+          if (lane == 0) put(i, below);
+        }
       }
     }
   }
@@ -236,22 +276,38 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, P
 // The parts of a row put together, a wavefront a row.
 template <typename T>
 __global__ __launch_bounds__(64) void logprobs_join_kernel(RowOut<T> row_out, PartOut part_out) {
+  constexpr int kRoomOfParts = 1024;
+  __shared__ unsigned long long candidates[kRoomOfParts];
   const int lane = threadIdx.x, k = row_out.k;
   const int64_t row = blockIdx.x;
   Stats mine = nothing();
   for (int p = lane; p < part_out.parts; p += 64) mine.join(part_out.stats[row * part_out.parts + p]);
   mine = wave_stats(mine);
   if (lane == 0) row_out.put(row, mine);
-  const unsigned long long* best = part_out.best + row * part_out.parts * k;
-  unsigned long long bar = ~0ull;
-  for (int i = 0; i < k; ++i) {
-    unsigned long long most = 0;
-    for (int n = lane; n < part_out.parts * k; n += 64) {
-      const unsigned long long r = best[n];
-      if (r < bar && r > most) most = r;
+  if (k == 0) return;
+  const int n = part_out.parts * k;
+  const unsigned long long* best = part_out.best + row * n;
+  if (n <= kRoomOfParts) {
+    int real = 0;
+    for (int i = lane; i < kRoomOfParts; i += 64) {
+      const unsigned long long r = i < n ? best[i] : 0;
+      candidates[i] = r;
+      real += __popcll(__ballot(r != 0));
     }
-    bar = wave_most(most);
-    if (lane == 0) row_out.put_alternative(row, i, bar, mine);
+    __syncthreads();
+    by_rank(candidates, n, k, lane, [&](int i, unsigned long long r) { row_out.put_alternative(row, i, r, mine); });
+    if (lane >= real && lane < k) row_out.put_alternative(row, lane, 0, mine);
+  } else {
+    unsigned long long below = ~0ull;
+    for (int i = 0; i < k; ++i) {
+      unsigned long long most = 0;
+      for (int j = lane; j < n; j += 64) {
+        const unsigned long long r = best[j];
+        if (r < below && r > most) most = r;
+      }
+      below = wave_most(most);
+      if (lane == 0) row_out.put_alternative(row, i, below, mine);
+    }
   }
 }
 
