@@ -27,7 +27,7 @@ constexpr int kMostAlternatives = 32;
 constexpr int kHeld = 64;                              // logits a lane keeps for the alternatives
 constexpr int64_t kHeldPart = (int64_t)kThreads * kHeld;
 
-__device__ __forceinline__ float held_back(float x) { return x < -1000.f ? -1000.f : x; }   // (NaN stays)
+__device__ __forceinline__ float held_back(float x) { return fmaxf(x, -1000.f); }   // (of what is no number -1000, and its e^x none)
 
 struct Stats {
   float m, s, w;
@@ -87,16 +87,14 @@ __device__ __forceinline__ unsigned long long wave_most(unsigned long long a) {
 
 constexpr int kRoom = 512;   // candidates in LDS
 
-// The k largest of n distinct candidates in LDS, by one wavefront: put(place, candidate) for those places that there are.
+// put(place, candidate) if the at-th of n distinct candidates in LDS is one of the k largest.
 template <typename P>
-__device__ __forceinline__ void by_rank(const unsigned long long* candidates, int n, int k, int lane, P put) {
-  for (int first = 0; first < n; first += 64) {
-    const unsigned long long mine = first + lane < n ? candidates[first + lane] : 0;
-    int larger = 0;
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) larger += candidates[i] > mine;
-    if (mine && larger < k) put(larger, mine);
-  }
+__device__ __forceinline__ void by_rank(const unsigned long long* candidates, int n, int k, int at, P put) {
+  const unsigned long long mine = at < n ? candidates[at] : 0;
+  int larger = 0;
+#pragma unroll 16
+  for (int i = 0; i < n; ++i) larger += candidates[i] > mine;
+  if (mine && larger < k) put(larger, mine);
 }
 
 struct PartOut {          // [row][part]
@@ -119,13 +117,17 @@ struct RowOut {
   int32_t* ids;
   float* alternatives;
 
-  // what lane 0 of a row's last wavefront writes
-  __device__ __forceinline__ void put(int64_t row, const Stats& a) const {
+  // the given token's logit; 0 and false if it has none
+  __device__ __forceinline__ float given(int64_t row, bool* is) const {
     const int64_t token = token_at(tokens, tokens64, row);
+    *is = token >= 0 && token < vocab;
+    return *is ? logit(logits[row * stride + token]) : 0.f;
+  }
+  __device__ __forceinline__ void put(int64_t row, const Stats& a, float x, bool is) const {
     const float ln = fast_log(a.s);
     const bool none = a.s == 0.f;
     float lp = 0.f;
-    if (token >= 0 && token < vocab) lp = none ? -INFINITY : (logit(logits[row * stride + token]) - a.m) - ln;
+    if (is) lp = none ? -INFINITY : (x - a.m) - ln;
     logprob[row] = a.s != a.s ? a.s : lp;
     entropy[row] = none ? 0.f : ln - a.w / a.s;
     lse[2 * row] = none ? 0.f : a.m;
@@ -141,7 +143,7 @@ struct RowOut {
 
 // One part of a row.  blockIdx.x: row * parts + part.  ALT: with alternatives, of at most kHeldPart logits.
 template <typename T, bool ALT>
-__global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
+__global__ __launch_bounds__(kThreads, 4) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
   constexpr int N = kWide<T>;
   __shared__ Stats wave_sums[kWaves];
   __shared__ unsigned long long candidates[ALT ? kRoom : 1];
@@ -150,12 +152,15 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, P
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = row_out.k;
   const int64_t row = blockIdx.x / part_out.parts, part = blockIdx.x % part_out.parts;
   const T* logits = row_out.logits + row * row_out.stride;
+  bool is_given = false;
+  const float given = part_out.parts == 1 ? row_out.given(row, &is_given) : 0.f;   // (on its way while the row is read)
   // pieces of 16 bytes that are aligned as such, the first and the last one cut off at the part's ends
   const int64_t begin = part * part_length, end = min(begin + part_length, row_out.vocab);
   const int64_t skew = (int64_t)((reinterpret_cast<uintptr_t>(logits + begin) & 15) / sizeof(T));
   Stats mine = nothing();
   constexpr int kPieces = kHeld / N + 1;   // (a piece more, since the first begins in front of the part)
-  Vec<T, N> held[ALT ? kPieces : 1];
+  using Held = Vec<T, N>;
+  Held held[ALT ? kPieces : 1];
   auto get = [&](int64_t at, T none) {     // logits at .. at + N - 1
     Vec<T, N> v;
     if (at >= begin && at + N <= end) {
@@ -166,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, P
     }
     return v;
   };
-  auto take = [&](const Vec<T, N>& v) {
+  auto take = [&](const Vec<T, N>& v) {   // returns the largest
     float x[N], most = -FLT_MAX;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -176,13 +181,15 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, P
     if (most > mine.m) mine.raise(most);
 #pragma unroll
     for (int i = 0; i < N; ++i) mine.add(x[i]);
+    return most;
   };
+  float tops[ALT ? kPieces : 1];   // of the pieces held
   const int64_t first = begin - skew + (int64_t)threadIdx.x * N;
   if constexpr (ALT) {
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) held[p] = get(first + (int64_t)p * kThreads * N, (T)-INFINITY);
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) take(held[p]);
+    for (int p = 0; p < kPieces; ++p) tops[p] = take(held[p]);
   } else {
     constexpr int kAhead = 4;
     for (int64_t at = first; at < end; at += kAhead * kThreads * N) {
@@ -196,16 +203,20 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, P
   float bar = -INFINITY;
   if constexpr (ALT) {
     // the lane's largest, and how many lanes' are larger (or as large, of lanes in front)
-    float most = -INFINITY;
+    float most = tops[0];
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-      for (int i = 0; i < N; ++i) most = fmaxf(most, (float)held[p].at[i]);
+    for (int p = 1; p < kPieces; ++p) most = fmaxf(most, tops[p]);
     int larger = 0;
 #pragma unroll
     for (int l = 0; l < 64; ++l) {
       const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(most), l));
       larger += other > most || (other == most && l < lane);
+    }
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {   // (what is looked at again is converted again: kept as 32-bit numbers it would take the registers of a wavefront)
+      Vec<unsigned, 4> words = __builtin_bit_cast(Vec<unsigned, 4>, held[p]);
+      asm volatile("" : "+v"(words.at[0]), "+v"(words.at[1]), "+v"(words.at[2]), "+v"(words.at[3]));
+      held[p] = __builtin_bit_cast(Held, words);
     }
     const unsigned long long at = __ballot(larger == k - 1);
     bar = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(most), __builtin_ctzll(at)));
@@ -220,10 +231,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, P
     for (int w = 0; w < kWaves; ++w) bar = fmaxf(bar, bars[w]);
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      float most = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < N; ++i) most = fmaxf(most, (float)held[p].at[i]);
-      if (most >= bar && most > -INFINITY) {
+      if (tops[p] >= bar) {
         const int64_t id = first + (int64_t)p * kThreads * N;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -244,7 +252,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, P
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) all.join(wave_sums[w]);
     if (lane == 0) {
-      if (whole) row_out.put(row, all);
+      if (whole) row_out.put(row, all, given, is_given);
       else part_out.stats[at] = all;
     }
     if constexpr (ALT) {
@@ -254,7 +262,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, P
         else part_out.best[at * k + i] = r;
       };
       if (n <= kRoom) {
-        by_rank(candidates, n, k, lane, put);
+        for (int first = 0; first < n; first += 64) by_rank(candidates, n, k, first + lane, put);
         if (lane >= n && lane < k) put(lane, 0);
       } else {
         unsigned long long below = ~0ull;
@@ -273,31 +281,43 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(RowOut<T> row_out, P
   }
 }
 
-// The parts of a row put together, a wavefront a row.
+// The parts of a row put together.
 template <typename T>
-__global__ __launch_bounds__(64) void logprobs_join_kernel(RowOut<T> row_out, PartOut part_out) {
+__global__ __launch_bounds__(kThreads) void logprobs_join_kernel(RowOut<T> row_out, PartOut part_out) {
   constexpr int kRoomOfParts = 1024;
   __shared__ unsigned long long candidates[kRoomOfParts];
-  const int lane = threadIdx.x, k = row_out.k;
+  __shared__ Stats all;
+  __shared__ int collected;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = row_out.k;
   const int64_t row = blockIdx.x;
-  Stats mine = nothing();
-  for (int p = lane; p < part_out.parts; p += 64) mine.join(part_out.stats[row * part_out.parts + p]);
-  mine = wave_stats(mine);
-  if (lane == 0) row_out.put(row, mine);
-  if (k == 0) return;
   const int n = part_out.parts * k;
   const unsigned long long* best = part_out.best + row * n;
+  if (threadIdx.x == 0) collected = 0;
+  __syncthreads();
   if (n <= kRoomOfParts) {
-    int real = 0;
-    for (int i = lane; i < kRoomOfParts; i += 64) {
-      const unsigned long long r = i < n ? best[i] : 0;
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const unsigned long long r = best[i];
       candidates[i] = r;
-      real += __popcll(__ballot(r != 0));
+      if (r) atomicAdd(&collected, 1);
     }
-    __syncthreads();
-    by_rank(candidates, n, k, lane, [&](int i, unsigned long long r) { row_out.put_alternative(row, i, r, mine); });
-    if (lane >= real && lane < k) row_out.put_alternative(row, lane, 0, mine);
-  } else {
+  }
+  if (wave == 0) {
+    bool is_given;
+    const float given = row_out.given(row, &is_given);
+    Stats mine = nothing();
+    for (int p = lane; p < part_out.parts; p += 64) mine.join(part_out.stats[row * part_out.parts + p]);
+    mine = wave_stats(mine);
+    if (lane == 0) {
+      all = mine;
+      row_out.put(row, mine, given, is_given);
+    }
+  }
+  __syncthreads();
+  if (n <= kRoomOfParts) {
+    for (int first = wave * 64; first < n; first += kThreads)
+      by_rank(candidates, n, k, first + lane, [&](int i, unsigned long long r) { row_out.put_alternative(row, i, r, all); });
+    if ((int)threadIdx.x >= collected && (int)threadIdx.x < k) row_out.put_alternative(row, threadIdx.x, 0, all);
+  } else if (wave == 0) {
     unsigned long long below = ~0ull;
     for (int i = 0; i < k; ++i) {
       unsigned long long most = 0;
@@ -306,7 +326,7 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(RowOut<T> row_out, Pa
         if (r < below && r > most) most = r;
       }
       below = wave_most(most);
-      if (lane == 0) row_out.put_alternative(row, i, below, mine);
+      if (lane == 0) row_out.put_alternative(row, i, below, all);
     }
   }
 }
@@ -408,7 +428,7 @@ int fpsched_op_logprobs(int device_id, int type, int64_t n_rows, int64_t vocab, 
     const dim3 grid((unsigned)(n_rows * p.parts));
     if (n_alternatives > 0) logprobs_kernel<T, true><<<grid, dim3(kThreads), 0, stream>>>(row, part, p.length);
     else logprobs_kernel<T, false><<<grid, dim3(kThreads), 0, stream>>>(row, part, p.length);
-    if (p.parts > 1) logprobs_join_kernel<T><<<dim3((unsigned)n_rows), dim3(64), 0, stream>>>(row, part);
+    if (p.parts > 1) logprobs_join_kernel<T><<<dim3((unsigned)n_rows), dim3(kThreads), 0, stream>>>(row, part);
     return launched();
   });
 }
