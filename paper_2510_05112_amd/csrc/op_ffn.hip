@@ -85,44 +85,68 @@ typedef __attribute__((address_space(3))) char lds_char;
 // A tile of ROWS m (or n) by kDepth k.  kAlong: [row][8 pieces of 8 k], piece p of row r in place p ^ (r / 2 % 8): of 16 rows that a read
 // takes one piece each, no two are in the same banks.  kDown: [k][ROWS / 8 pieces of 8 rows], piece p of k in place p ^ (k % 4 * 4): the
 // four k of a transposing read are in different quarters of the banks.
-template <int LAYOUT, int ROWS, int THREADS>
+//
+// A thread loads kLoads pieces of it; they are the same number of rows (or k) apart, so that one offset serves all, and what differs is the
+// same for all lanes.  HALVES: rows from ROWS / 2 on are those of another place, n_half rows on.
+template <int LAYOUT, int ROWS, int THREADS, bool HALVES>
 struct Tile {
   static constexpr int kBytes = ROWS * kDepth * 2, kLoads = kBytes / 16 / THREADS;
+  static constexpr int kPieces = LAYOUT == kAlong ? kDepth / 8 : ROWS / 8;       // in a row of LDS
+  static constexpr int kApart = THREADS / kPieces;                               // rows of LDS between a thread's loads
+  static constexpr int kHalfLoads = HALVES ? kLoads / 2 : kLoads;
+  static_assert(kLoads * kApart == (LAYOUT == kAlong ? ROWS : kDepth) && (LAYOUT == kAlong ? kApart % 16 == 0 : kApart % 4 == 0), "places do not depend on the load");
 
-  // The tile's part of an operand at rows `row0`, k `k0`, to LDS.  half: rows from ROWS / 2 on are those of another place, half_row0.
-  template <bool HALVES>
-  static __device__ __forceinline__ void load(const Operand& o, int64_t row0, int64_t half_row0, int64_t half_extent, int64_t k0, int64_t depth,
-                                              char* lds, int thread) {
-    const int wave = thread >> 6;
-    const int64_t k_left = min(depth - k0, (int64_t)kDepth);
+  const char *base, *half_base;   // of the next tile to load
+  int records, half_records;      // bytes from there to the operand's end, as far as this tile's rows go
+  int64_t step;                   // bytes to the tile behind it
+  int apart, last_records;
+  unsigned offset, last_offset;
+
+  __device__ __forceinline__ void begin(const Operand& o, int64_t row0, int64_t n_half, int64_t depth, int thread) {
+    const int r = thread / kPieces, place = thread % kPieces;
+    const int stride = (int)o.stride, last_k = (int)((depth - 1) % kDepth) + 1;
+    apart = kApart * stride * 2;
+    if constexpr (LAYOUT == kAlong) {
+      const int piece = place ^ (r >> 1 & 7);
+      base = static_cast<const char*>(o.data) + row0 * o.stride * 2;
+      half_base = base + n_half * o.stride * 2;
+      const int64_t end = HALVES ? n_half : o.extent;
+      const int rows = (int)min(end - row0, (int64_t)(HALVES ? ROWS / 2 : ROWS));
+      records = half_records = ((rows - 1) * stride + (int)depth) * 2;
+      step = kDepth * 2;
+      last_records = 0;
+      offset = (unsigned)(r * stride + piece * 8) * 2;
+      last_offset = piece * 8 < last_k ? offset : kOutside;
+    } else {
+      const int piece = place ^ ((r & 3) << 2);
+      const int left = (int)min(o.extent - row0, (int64_t)ROWS);
+      base = half_base = static_cast<const char*>(o.data) + row0 * 2;
+      records = half_records = ((kDepth - 1) * stride + left) * 2;
+      last_records = ((last_k - 1) * stride + left) * 2;
+      step = (int64_t)kDepth * stride * 2;
+      offset = last_offset = piece * 8 < left ? (unsigned)(r * stride + piece * 8) * 2 : kOutside;
+    }
+  }
+
+  // The next tile to LDS.  last: it is the last one.
+  __device__ __forceinline__ void load(char* lds, int wave, bool last) {
+    if (LAYOUT == kDown && last) records = last_records;
+    const unsigned from = last ? last_offset : offset;
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, records, 0x00027000);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int q = i * THREADS + thread;
-      unsigned offset;
-      const char* base;
-      int64_t bytes;
-      if constexpr (LAYOUT == kAlong) {
-        constexpr int kRows = HALVES ? ROWS / 2 : ROWS, kRowsOfLoad = THREADS / 8;
-        static_assert(kRows % kRowsOfLoad == 0, "a load is in one half");
-        const int r = q >> 3, piece = (q & 7) ^ (r >> 1 & 7);
-        const bool second = i * kRowsOfLoad >= kRows;   // (a constant)
-        const int64_t first = second ? half_row0 : row0, end = HALVES && !second ? half_extent : o.extent;
-        const int64_t rows = max(min(end - first, (int64_t)kRows), (int64_t)0);
-        base = static_cast<const char*>(o.data) + (first * o.stride + k0) * 2;
-        bytes = rows > 0 ? ((rows - 1) * o.stride + k_left) * 2 : 0;
-        offset = (unsigned)((second ? r - kRows : r) * (int)o.stride + piece * 8) * 2;
-        if (piece * 8 >= k_left) offset = kOutside;
-      } else {
-        constexpr int kPieces = ROWS / 8;
-        const int k = q / kPieces, piece = (q % kPieces) ^ ((k & 3) << 2);
-        const int64_t left = o.extent - row0;
-        base = static_cast<const char*>(o.data) + (k0 * o.stride + row0) * 2;
-        bytes = ((k_left - 1) * o.stride + left) * 2;
-        offset = (unsigned)(k * (int)o.stride + piece * 8) * 2;
-        if (piece * 8 >= left) offset = kOutside;
-      }
-      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)min(bytes, (int64_t)0x7fffffff), 0x00027000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_char*)(lds + (i * THREADS + wave * 64) * 16), 16, (int)offset, 0, 0, 0);
+    for (int i = 0; i < kHalfLoads; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_char*)(lds + (i * THREADS + wave * 64) * 16), 16, (int)from, i * apart, 0, 0);
+    base += step;
+    if constexpr (HALVES) {
+      const __amdgpu_buffer_rsrc_t half = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(half_base), 0, half_records, 0x00027000);
+#pragma unroll
+      for (int i = 0; i < kHalfLoads; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(half, (lds_char*)(lds + ((i + kHalfLoads) * THREADS + wave * 64) * 16), 16, (int)from, i * apart, 0, 0);
+      half_base += step;
+    }
+    if constexpr (LAYOUT == kAlong) {
+      records -= kDepth * 2;
+      half_records -= kDepth * 2;
     }
   }
 
@@ -154,97 +178,151 @@ __device__ __forceinline__ void tile_of(unsigned id, int tiles_m, int tiles_n, i
   *tn = in / high;
 }
 
+// What becomes of 8 neighbouring columns of a row.
+template <typename T, int EPILOGUE, typename O>
+__device__ __forceinline__ void put_columns(const Gemm& a, int64_t m, int64_t n, const Vec<float, 8>& x) {
+  if constexpr (EPILOGUE == kGatedGrad) {
+    const T* pre = static_cast<const T*>(a.pre) + m * 2 * a.n_half + n;
+    const Vec<T, 8> g = load_vec<T, 8>(pre), u = load_vec<T, 8>(pre + a.n_half);
+    Vec<T, 8> dg, du;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float gate = (float)g.at[e];
+      dg.at[e] = (T)(x.at[e] * (float)u.at[e] * slope(a.act, gate));
+      du.at[e] = (T)(x.at[e] * activate(a.act, gate));
+    }
+    T* out = static_cast<T*>(a.out) + m * a.out_stride + n;
+    store_vec<T, 8>(out, dg);
+    store_vec<T, 8>(out + a.n_half, du);
+  } else {
+    O* out = static_cast<O*>(a.out) + m * a.out_stride + n;
+    Vec<O, 8> v = {};
+    if (std::is_same<O, float>::value && a.accumulate) {
+      const Vec<O, 4> low = load_vec<O, 4>(out), high = load_vec<O, 4>(out + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v.at[e] = low.at[e], v.at[e + 4] = high.at[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v.at[e] = (O)((float)v.at[e] + x.at[e]);
+    if constexpr (std::is_same<O, float>::value) {   // (rows begin at 16 bytes)
+      store_vec<O, 4>(out, {v.at[0], v.at[1], v.at[2], v.at[3]});
+      store_vec<O, 4>(out + 4, {v.at[4], v.at[5], v.at[6], v.at[7]});
+    } else {
+      store_vec<O, 8>(out, v);
+    }
+  }
+}
+
 template <typename T, int LM, int LN, int EPILOGUE, typename O, int BM, int BN>
 __global__ __launch_bounds__(BN * 2) void gemm_kernel(Gemm a) {
   constexpr int kThreads = BN * 2;                         // (a wavefront for 64 columns of half of the rows)
-  constexpr int kWavesN = BN / 64, MF = BM / 64, NF = 2;
-  using TileM = Tile<LM, BM, kThreads>;
-  using TileN = Tile<LN, BN, kThreads>;
+  constexpr int kWavesN = BN / 64, MF = BM / 64, NF = 2, kStepsOfTile = kDepth / 16;
   constexpr bool kHalves = EPILOGUE == kGated;
-  __shared__ __align__(1024) char lds[2][TileM::kBytes + TileN::kBytes];
+  using TileM = Tile<LM, BM, kThreads, false>;
+  using TileN = Tile<LN, BN, kThreads, kHalves>;
+  constexpr int kTile = TileM::kBytes + TileN::kBytes;
+  __shared__ __align__(1024) char lds[2 * kTile];
   const int thread = threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int wave_m = wave / kWavesN, wave_n = wave % kWavesN;
   int tm, tn;
   tile_of(blockIdx.x, a.tiles_m, a.tiles_n, &tm, &tn);
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * (kHalves ? BN / 2 : BN);
   f32x16 acc[MF][NF] = {};
-  auto load = [&](int64_t k0, char* to) {
-    TileM::template load<false>(a.m, m0, 0, 0, k0, a.depth, to, thread);
-    TileN::template load<kHalves>(a.n, n0, a.n_half + n0, a.n_half, k0, a.depth, to + TileM::kBytes, thread);
+  const int tiles = (int)((a.depth + kDepth - 1) / kDepth);
+  TileM tile_m;
+  TileN tile_n;
+  tile_m.begin(a.m, m0, 0, a.depth, thread);
+  tile_n.begin(a.n, n0, a.n_half, a.depth, thread);
+  auto load = [&](int t) {
+    char* to = lds + (t & 1) * kTile;
+    tile_m.load(to, wave, t == tiles - 1);
+    tile_n.load(to + TileM::kBytes, wave, t == tiles - 1);
   };
-  load(0, lds[0]);
-  int buffer = 0;
-  for (int64_t k0 = 0; k0 < a.depth; k0 += kDepth, buffer ^= 1) {
-    __syncthreads();   // this tile has arrived, and the other buffer's has been read
-    if (k0 + kDepth < a.depth) load(k0 + kDepth, lds[buffer ^ 1]);
-    const char *at_m = lds[buffer], *at_n = lds[buffer] + TileM::kBytes;
+  typename Frag<T>::type fm[2][MF], fn[2][NF];
+  auto read = [&](int t, int step, int which) {
+    const char *at_m = lds + (t & 1) * kTile, *at_n = at_m + TileM::kBytes;
 #pragma unroll
-    for (int step = 0; step < kDepth / 16; ++step) {
-      typename Frag<T>::type fm[MF], fn[NF];
+    for (int j = 0; j < NF; ++j) fn[which][j] = TileN::template frag<T>(at_n, kHalves ? j * (BN / 2) + wave_n * 32 : (wave_n * NF + j) * 32, step, lane);
 #pragma unroll
-      for (int i = 0; i < MF; ++i) fm[i] = TileM::template frag<T>(at_m, (wave_m * MF + i) * 32, step, lane);
+    for (int i = 0; i < MF; ++i) fm[which][i] = TileM::template frag<T>(at_m, (wave_m * MF + i) * 32, step, lane);
+  };
+  auto multiply = [&](int which) {
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int j = 0; j < NF; ++j) fn[j] = TileN::template frag<T>(at_n, kHalves ? j * (BN / 2) + wave_n * 32 : (wave_n * NF + j) * 32, step, lane);
+    for (int i = 0; i < MF; ++i)
 #pragma unroll
-      for (int i = 0; i < MF; ++i)
+      for (int j = 0; j < NF; ++j) acc[i][j] = Frag<T>::mul(fn[which][j], fm[which][i], acc[i][j]);
+    __builtin_amdgcn_s_setprio(0);
+  };
+  // A step's fragments are read while the one in front of it is multiplied.  When the last ones of a tile have been read, its place in LDS
+  // goes to the tile after the next one, which then has a whole tile's products to arrive.
+  load(0);
+  __syncthreads();
+  if (tiles > 1) load(1);
+  read(0, 0, 0);
+  for (int t = 0; t < tiles; ++t) {
 #pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = Frag<T>::mul(fn[j], fm[i], acc[i][j]);
+    for (int step = 0; step < kStepsOfTile - 1; ++step) {
+      read(t, step + 1, (step + 1) & 1);
+      multiply(step & 1);
     }
+    __syncthreads();
+    if (t + 2 < tiles) load(t + 2);
+    if (t + 1 < tiles) read(t + 1, 0, 0);
+    multiply((kStepsOfTile - 1) & 1);
   }
+  // A wavefront's 32 rows at a time go through LDS, so that rows are read and written 8 columns a lane.
+  constexpr int kPad = 68;   // floats between rows: 16 rows' pieces of 16 bytes are in different banks
+  __syncthreads();
+  float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kPad;
+  static_assert(kThreads / 64 * 32 * kPad * 4 <= 2 * kTile, "the rows fit");
 #pragma unroll
   for (int i = 0; i < MF; ++i) {
-    const int64_t m = m0 + (wave_m * MF + i) * 32 + (lane & 31);
-    if (m >= a.m.extent) continue;
+#pragma unroll
+    for (int j = 0; j < NF; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        store_vec<float, 4>(mine + (lane & 31) * kPad + j * 32 + q * 8 + (lane >> 5) * 4,
+                            {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]});
+    __builtin_amdgcn_wave_barrier();
+    const int64_t rows = m0 + (wave_m * MF + i) * 32;
     if constexpr (EPILOGUE == kGated) {
+      const int64_t f = n0 + wave_n * 32 + (lane & 3) * 8;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t f = n0 + wave_n * 32 + q * 8 + (lane >> 5) * 4;   // (a multiple of 4, as is their number)
-        if (f >= a.n_half) continue;
-        Vec<T, 4> h, g, u;
+      for (int p = 0; p < 2; ++p) {
+        const int r = p * 16 + (lane >> 2);
+        const int64_t m = rows + r;
+        const float* from = mine + r * kPad + (lane & 3) * 8;
+        const Vec<float, 4> g0 = load_vec<float, 4>(from), g1 = load_vec<float, 4>(from + 4), u0 = load_vec<float, 4>(from + 32), u1 = load_vec<float, 4>(from + 36);
+        if (m >= a.m.extent || f >= a.n_half) continue;
+        Vec<T, 8> h, g, u;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float gate = acc[i][0][q * 4 + e], up = acc[i][1][q * 4 + e];
+        for (int e = 0; e < 8; ++e) {
+          const float gate = e < 4 ? g0.at[e] : g1.at[e - 4], up = e < 4 ? u0.at[e] : u1.at[e - 4];
           h.at[e] = (T)(activate(a.act, gate) * up);
           g.at[e] = (T)gate;
           u.at[e] = (T)up;
         }
-        store_vec<T, 4>(static_cast<T*>(a.out) + m * a.out_stride + f, h);
+        store_vec<T, 8>(static_cast<T*>(a.out) + m * a.out_stride + f, h);
         if (a.pre) {
           T* pre = static_cast<T*>(a.pre) + m * 2 * a.n_half + f;
-          store_vec<T, 4>(pre, g);
-          store_vec<T, 4>(pre + a.n_half, u);
+          store_vec<T, 8>(pre, g);
+          store_vec<T, 8>(pre + a.n_half, u);
         }
       }
     } else {
+      const int64_t n = n0 + wave_n * 64 + (lane & 7) * 8;
 #pragma unroll
-      for (int j = 0; j < NF; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int64_t n = n0 + (wave_n * NF + j) * 32 + q * 8 + (lane >> 5) * 4;
-          if (n >= a.n.extent) continue;
-          if constexpr (EPILOGUE == kGatedGrad) {
-            const T* pre = static_cast<const T*>(a.pre) + m * 2 * a.n_half + n;
-            const Vec<T, 4> g = load_vec<T, 4>(pre), u = load_vec<T, 4>(pre + a.n_half);
-            Vec<T, 4> dg, du;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float d = acc[i][j][q * 4 + e], gate = (float)g.at[e];
-              dg.at[e] = (T)(d * (float)u.at[e] * slope(a.act, gate));
-              du.at[e] = (T)(d * activate(a.act, gate));
-            }
-            T* out = static_cast<T*>(a.out) + m * a.out_stride + n;
-            store_vec<T, 4>(out, dg);
-            store_vec<T, 4>(out + a.n_half, du);
-          } else {
-            O* out = static_cast<O*>(a.out) + m * a.out_stride + n;
-            Vec<O, 4> v = {};
-            if (std::is_same<O, float>::value && a.accumulate) v = load_vec<O, 4>(out);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v.at[e] = (O)((float)v.at[e] + acc[i][j][q * 4 + e]);
-            store_vec<O, 4>(out, v);
-          }
-        }
+      for (int p = 0; p < 4; ++p) {
+        const int r = p * 8 + (lane >> 3);
+        const int64_t m = rows + r;
+        const float* from = mine + r * kPad + (lane & 7) * 8;
+        const Vec<float, 4> x0 = load_vec<float, 4>(from), x1 = load_vec<float, 4>(from + 4);
+        if (m >= a.m.extent || n >= a.n.extent) continue;
+        put_columns<T, EPILOGUE, O>(a, m, n, {x0.at[0], x0.at[1], x0.at[2], x0.at[3], x1.at[0], x1.at[1], x1.at[2], x1.at[3]});
+      }
     }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
