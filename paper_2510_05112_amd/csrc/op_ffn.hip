@@ -129,19 +129,19 @@ struct Tile {
   }
 
   // The next tile to LDS.  last: it is the last one.
-  __device__ __forceinline__ void load(char* lds, int wave, bool last) {
+  __device__ __forceinline__ void load(lds_char* lds, int wave, bool last) {
     if (LAYOUT == kDown && last) records = last_records;
     const unsigned from = last ? last_offset : offset;
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, records, 0x00027000);
 #pragma unroll
     for (int i = 0; i < kHalfLoads; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_char*)(lds + (i * THREADS + wave * 64) * 16), 16, (int)from, i * apart, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, lds + (i * THREADS + wave * 64) * 16, 16, (int)from, i * apart, 0, 0);
     base += step;
     if constexpr (HALVES) {
       const __amdgpu_buffer_rsrc_t half = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(half_base), 0, half_records, 0x00027000);
 #pragma unroll
       for (int i = 0; i < kHalfLoads; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(half, (lds_char*)(lds + ((i + kHalfLoads) * THREADS + wave * 64) * 16), 16, (int)from, i * apart, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(half, lds + ((i + kHalfLoads) * THREADS + wave * 64) * 16, 16, (int)from, i * apart, 0, 0);
       half_base += step;
     }
     if constexpr (LAYOUT == kAlong) {
@@ -152,10 +152,11 @@ struct Tile {
 
   // A lane's 8 k (16 step + 8 (lane / 32) ...) of row first + lane % 32.
   template <typename T>
-  static __device__ __forceinline__ typename Frag<T>::type frag(const char* lds, int first, int step, int lane) {
+  static __device__ __forceinline__ typename Frag<T>::type frag(const lds_char* lds, int first, int step, int lane) {
     if constexpr (LAYOUT == kAlong) {
       const int r = first + (lane & 31), piece = step * 2 + (lane >> 5);
-      return *reinterpret_cast<const typename Frag<T>::type*>(lds + r * (kDepth * 2) + ((piece ^ (r >> 1 & 7)) << 4));
+      typedef __attribute__((address_space(3))) const typename Frag<T>::type lds_frag;
+      return *(lds_frag*)(lds + r * (kDepth * 2) + ((piece ^ (r >> 1 & 7)) << 4));
     } else {
       const int k = step * 16 + (lane >> 5) * 8 + (lane >> 2 & 3), column = first + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
       const int place = ((column >> 3) ^ ((k & 3) << 2)) * 16 + (column & 7) * 2;
@@ -233,19 +234,11 @@ __global__ __launch_bounds__(BN * 2) void gemm_kernel(Gemm a) {
   TileN tile_n;
   tile_m.begin(a.m, m0, 0, a.depth, thread);
   tile_n.begin(a.n, n0, a.n_half, a.depth, thread);
-  auto load = [&](int t) {
-    char* to = lds + (t & 1) * kTile;
+  auto load = [&](int t, lds_char* to) {
     tile_m.load(to, wave, t == tiles - 1);
     tile_n.load(to + TileM::kBytes, wave, t == tiles - 1);
   };
-  typename Frag<T>::type fm[2][MF], fn[2][NF];
-  auto read = [&](int t, int step, int which) {
-    const char *at_m = lds + (t & 1) * kTile, *at_n = at_m + TileM::kBytes;
-#pragma unroll
-    for (int j = 0; j < NF; ++j) fn[which][j] = TileN::template frag<T>(at_n, kHalves ? j * (BN / 2) + wave_n * 32 : (wave_n * NF + j) * 32, step, lane);
-#pragma unroll
-    for (int i = 0; i < MF; ++i) fm[which][i] = TileM::template frag<T>(at_m, (wave_m * MF + i) * 32, step, lane);
-  };
+  typename Frag<T>::type fm[2][MF] = {}, fn[2][NF] = {};
   auto multiply = [&](int which) {
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -254,23 +247,29 @@ __global__ __launch_bounds__(BN * 2) void gemm_kernel(Gemm a) {
       for (int j = 0; j < NF; ++j) acc[i][j] = Frag<T>::mul(fn[which][j], fm[which][i], acc[i][j]);
     __builtin_amdgcn_s_setprio(0);
   };
-  // A step's fragments are read while the one in front of it is multiplied.  When the last ones of a tile have been read, its place in LDS
-  // goes to the tile after the next one, which then has a whole tile's products to arrive.
-  load(0);
-  __syncthreads();
-  if (tiles > 1) load(1);
-  read(0, 0, 0);
-  for (int t = 0; t < tiles; ++t) {
+  // A step's fragments are read while the one in front of it is multiplied, the first ones of a tile while the last ones of the tile
+  // before are.  When those have been read, that tile's place in LDS goes to the tile after this one, which has all of this one's products to arrive.
+  // (That the two places are different ones is said by __restrict: the compiler would else wait for what is on its way to one in front of
+  // each transposing read of the other.)
+  auto work_on = [&](int t, lds_char* __restrict place, lds_char* __restrict next) __attribute__((always_inline)) {
+    if (t + 1 < tiles) load(t + 1, next);
 #pragma unroll
-    for (int step = 0; step < kStepsOfTile - 1; ++step) {
-      read(t, step + 1, (step + 1) & 1);
-      multiply(step & 1);
+    for (int step = 0; step < kStepsOfTile; ++step) {
+#pragma unroll
+      for (int j = 0; j < NF; ++j)
+        fn[step & 1][j] = TileN::template frag<T>(place + TileM::kBytes, kHalves ? j * (BN / 2) + wave_n * 32 : (wave_n * NF + j) * 32, step, lane);
+#pragma unroll
+      for (int i = 0; i < MF; ++i) fm[step & 1][i] = TileM::template frag<T>(place, (wave_m * MF + i) * 32, step, lane);
+      multiply((step + 1) & 1);   // (in the first tile's first step, zeros)
     }
-    __syncthreads();
-    if (t + 2 < tiles) load(t + 2);
-    if (t + 1 < tiles) read(t + 1, 0, 0);
-    multiply((kStepsOfTile - 1) & 1);
+  };
+  lds_char* const room = (lds_char*)lds;
+  load(0, room);
+  for (int t = 0; t < tiles; ++t) {
+    __syncthreads();   // this tile has arrived, and the other place has been read
+    work_on(t, room + (t & 1) * kTile, room + ((t + 1) & 1) * kTile);
   }
+  multiply((kStepsOfTile - 1) & 1);
   // A wavefront's 32 rows at a time go through LDS, so that rows are read and written 8 columns a lane.
   constexpr int kPad = 68;   // floats between rows: 16 rows' pieces of 16 bytes are in different banks
   __syncthreads();
