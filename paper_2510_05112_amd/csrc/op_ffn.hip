@@ -82,8 +82,8 @@ __device__ __forceinline__ float slope(int act, float g) {
 
 typedef __attribute__((address_space(3))) char lds_char;
 
-// A tile of ROWS m (or n) by kDepth k.  kAlong: [row][8 pieces of 8 k], piece p of row r in place p ^ (r / 2 % 8): of 16 rows that a read
-// takes one piece each, no two are in the same banks.  kDown: [k][ROWS / 8 pieces of 8 rows], piece p of k in place p ^ (k % 4 * 4): the
+// A tile of ROWS m (or n) by kDepth k.  kAlong: [row][8 pieces of 8 k], piece p of row r in place p ^ (r / 2 % 8): of 16
+// rows that a read takes one piece each, no two are in the same banks.  kDown: [k][ROWS / 8 pieces of 8 rows], piece p of k in place p ^ (k % 4 * 4): the
 // four k of a transposing read are in different quarters of the banks.
 //
 // A thread loads kLoads pieces of it; they are the same number of rows (or k) apart, so that one offset serves all, and what differs is the
@@ -97,7 +97,7 @@ struct Tile {
   static_assert(kLoads * kApart == (LAYOUT == kAlong ? ROWS : kDepth) && (LAYOUT == kAlong ? kApart % 16 == 0 : kApart % 4 == 0), "places do not depend on the load");
 
   const char *base, *half_base;   // of the next tile to load
-  int records, half_records;      // bytes from there to the operand's end, as far as this tile's rows go
+  int records;                    // bytes from there to the operand's end, as far as this tile's rows go
   int64_t step;                   // bytes to the tile behind it
   int apart, last_records;
   unsigned offset, last_offset;
@@ -112,7 +112,7 @@ struct Tile {
       half_base = base + n_half * o.stride * 2;
       const int64_t end = HALVES ? n_half : o.extent;
       const int rows = (int)min(end - row0, (int64_t)(HALVES ? ROWS / 2 : ROWS));
-      records = half_records = ((rows - 1) * stride + (int)depth) * 2;
+      records = ((rows - 1) * stride + (int)depth) * 2;
       step = kDepth * 2;
       last_records = 0;
       offset = (unsigned)(r * stride + piece * 8) * 2;
@@ -121,33 +121,34 @@ struct Tile {
       const int piece = place ^ ((r & 3) << 2);
       const int left = (int)min(o.extent - row0, (int64_t)ROWS);
       base = half_base = static_cast<const char*>(o.data) + row0 * 2;
-      records = half_records = ((kDepth - 1) * stride + left) * 2;
+      records = ((kDepth - 1) * stride + left) * 2;
       last_records = ((last_k - 1) * stride + left) * 2;
       step = (int64_t)kDepth * stride * 2;
       offset = last_offset = piece * 8 < left ? (unsigned)(r * stride + piece * 8) * 2 : kOutside;
     }
   }
 
-  // The next tile to LDS.  last: it is the last one.
-  __device__ __forceinline__ void load(lds_char* lds, int wave, bool last) {
-    if (LAYOUT == kDown && last) records = last_records;
-    const unsigned from = last ? last_offset : offset;
-    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, records, 0x00027000);
-#pragma unroll
-    for (int i = 0; i < kHalfLoads; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, lds + (i * THREADS + wave * 64) * 16, 16, (int)from, i * apart, 0, 0);
+  __amdgpu_buffer_rsrc_t rsrc, half_rsrc;   // of the tile that is being loaded
+  unsigned from;
+
+  // Goes on to the next tile to load.  last: it is the last one; none: there is none, and what is loaded is zeros.
+  __device__ __forceinline__ void next(bool last, bool none) {
+    const int bytes = none ? 0 : LAYOUT == kDown && last ? last_records : records;
+    from = last ? last_offset : offset;
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, bytes, 0x00027000);
     base += step;
     if constexpr (HALVES) {
-      const __amdgpu_buffer_rsrc_t half = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(half_base), 0, half_records, 0x00027000);
-#pragma unroll
-      for (int i = 0; i < kHalfLoads; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(half, lds + ((i + kHalfLoads) * THREADS + wave * 64) * 16, 16, (int)from, i * apart, 0, 0);
+      half_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(half_base), 0, bytes, 0x00027000);
       half_base += step;
     }
-    if constexpr (LAYOUT == kAlong) {
-      records -= kDepth * 2;
-      half_records -= kDepth * 2;
-    }
+    if constexpr (LAYOUT == kAlong) records -= kDepth * 2;
+  }
+  // One of its kLoads pieces for each thread.
+  __device__ __forceinline__ void load(lds_char* lds, int wave, int i) {
+    if (HALVES && i >= kHalfLoads)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(half_rsrc, lds + (i * THREADS + wave * 64) * 16, 16, (int)from, (i - kHalfLoads) * apart, 0, 0);
+    else
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, lds + (i * THREADS + wave * 64) * 16, 16, (int)from, i * apart, 0, 0);
   }
 
   // A lane's 8 k (16 step + 8 (lane / 32) ...) of row first + lane % 32.
@@ -214,10 +215,17 @@ __device__ __forceinline__ void put_columns(const Gemm& a, int64_t m, int64_t n,
   }
 }
 
-template <typename T, int LM, int LN, int EPILOGUE, typename O, int BM, int BN>
-__global__ __launch_bounds__(BN * 2) void gemm_kernel(Gemm a) {
-  constexpr int kThreads = BN * 2;                         // (a wavefront for 64 columns of half of the rows)
-  constexpr int kWavesN = BN / 64, MF = BM / 64, NF = 2, kStepsOfTile = kDepth / 16;
+// All wavefronts of a workgroup have read what they read of LDS, and their loads to it have arrived.
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" : : : "memory");
+}
+
+template <typename T, int LM, int LN, int EPILOGUE, typename O, int BM, int BN, int kWavesM, int kWavesN>
+__global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
+  constexpr int kThreads = kWavesM * kWavesN * 64;
+  constexpr int MF = BM / kWavesM / 32, NF = BN / kWavesN / 32, kStepsOfTile = kDepth / 16;
   constexpr bool kHalves = EPILOGUE == kGated;
   using TileM = Tile<LM, BM, kThreads, false>;
   using TileN = Tile<LN, BN, kThreads, kHalves>;
@@ -234,44 +242,56 @@ __global__ __launch_bounds__(BN * 2) void gemm_kernel(Gemm a) {
   TileN tile_n;
   tile_m.begin(a.m, m0, 0, a.depth, thread);
   tile_n.begin(a.n, n0, a.n_half, a.depth, thread);
-  auto load = [&](int t, lds_char* to) {
-    tile_m.load(to, wave, t == tiles - 1);
-    tile_n.load(to + TileM::kBytes, wave, t == tiles - 1);
-  };
   typename Frag<T>::type fm[2][MF] = {}, fn[2][NF] = {};
-  auto multiply = [&](int which) {
-    __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-    for (int i = 0; i < MF; ++i)
-#pragma unroll
-      for (int j = 0; j < NF; ++j) acc[i][j] = Frag<T>::mul(fn[which][j], fm[which][i], acc[i][j]);
-    __builtin_amdgcn_s_setprio(0);
+  constexpr int kLoads = TileM::kLoads + TileN::kLoads;
+  auto load = [&](lds_char* to, int i) {
+    if (i < TileM::kLoads) tile_m.load(to, wave, i);
+    else tile_n.load(to + TileM::kBytes, wave, i - TileM::kLoads);
   };
-  // A step's fragments are read while the one in front of it is multiplied, the first ones of a tile while the last ones of the tile
-  // before are.  When those have been read, that tile's place in LDS goes to the tile after this one, which has all of this one's products to arrive.
+  auto next_tile = [&](int t) {
+    tile_m.next(t == tiles - 1, t >= tiles);
+    tile_n.next(t == tiles - 1, t >= tiles);
+  };
+  // A step's fragments are read between the products of the one in front of it, the first ones of a tile between the last products of the
+  // tile before, and the next tile's loads are issued between the first of a tile's products: any of them by itself would keep a wavefront from
+  // its products for as long as the wavefronts of the compute unit need to issue theirs.
   // (That the two places are different ones is said by __restrict: the compiler would else wait for what is on its way to one in front of
   // each transposing read of the other.)
-  auto work_on = [&](int t, lds_char* __restrict place, lds_char* __restrict next) __attribute__((always_inline)) {
-    if (t + 1 < tiles) load(t + 1, next);
+  auto work_on = [&](int t, lds_char* __restrict place, lds_char* __restrict other) __attribute__((always_inline)) {
+    next_tile(t + 1);
 #pragma unroll
     for (int step = 0; step < kStepsOfTile; ++step) {
+      const int to = step & 1, of = to ^ 1;   // fragments to read, to multiply (in the first tile's first step, zeros)
 #pragma unroll
       for (int j = 0; j < NF; ++j)
-        fn[step & 1][j] = TileN::template frag<T>(place + TileM::kBytes, kHalves ? j * (BN / 2) + wave_n * 32 : (wave_n * NF + j) * 32, step, lane);
+        fn[to][j] = TileN::template frag<T>(place + TileM::kBytes, kHalves ? j / (NF / 2) * (BN / 2) + (wave_n * (NF / 2) + j % (NF / 2)) * 32 : (wave_n * NF + j) * 32, step, lane);
 #pragma unroll
-      for (int i = 0; i < MF; ++i) fm[step & 1][i] = TileM::template frag<T>(place, (wave_m * MF + i) * 32, step, lane);
-      multiply((step + 1) & 1);   // (in the first tile's first step, zeros)
+      for (int i = 0; i < MF; ++i) {
+        fm[to][i] = TileM::template frag<T>(place, (wave_m * MF + i) * 32, step, lane);
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = Frag<T>::mul(fn[of][j], fm[of][i], acc[i][j]);
+        constexpr int kTurns = MF;   // of products among which the loads are spread: a step's (over a tile's they come late: 7 % slower)
+        const int turn = step * MF + i;
+#pragma unroll
+        for (int l = turn * kLoads / kTurns; l < (turn + 1) * kLoads / kTurns && l < kLoads; ++l) load(other, l);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   };
   lds_char* const room = (lds_char*)lds;
-  load(0, room);
+  next_tile(0);
+#pragma unroll
+  for (int l = 0; l < kLoads; ++l) load(room, l);
   for (int t = 0; t < tiles; ++t) {
-    __syncthreads();   // this tile has arrived, and the other place has been read
+    meet();
     work_on(t, room + (t & 1) * kTile, room + ((t + 1) & 1) * kTile);
   }
-  multiply((kStepsOfTile - 1) & 1);
+#pragma unroll
+  for (int i = 0; i < MF; ++i)
+#pragma unroll
+    for (int j = 0; j < NF; ++j) acc[i][j] = Frag<T>::mul(fn[(kStepsOfTile - 1) & 1][j], fm[(kStepsOfTile - 1) & 1][i], acc[i][j]);
   // A wavefront's 32 rows at a time go through LDS, so that rows are read and written 8 columns a lane.
-  constexpr int kPad = 68;   // floats between rows: 16 rows' pieces of 16 bytes are in different banks
+  constexpr int kPad = NF * 32 + 4;   // floats between rows: 16 rows' pieces of 16 bytes are in different banks
   __syncthreads();
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kPad;
   static_assert(kThreads / 64 * 32 * kPad * 4 <= 2 * kTile, "the rows fit");
@@ -285,38 +305,32 @@ __global__ __launch_bounds__(BN * 2) void gemm_kernel(Gemm a) {
                             {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]});
     __builtin_amdgcn_wave_barrier();
     const int64_t rows = m0 + (wave_m * MF + i) * 32;
-    if constexpr (EPILOGUE == kGated) {
-      const int64_t f = n0 + wave_n * 32 + (lane & 3) * 8;
+    constexpr int kColumns = (kHalves ? NF / 2 : NF) * 32, kLanes = kColumns / 8, kRows = 64 / kLanes;   // of the output; lanes of a row, rows at a time
+    const int64_t n = n0 + wave_n * kColumns + lane % kLanes * 8;
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int r = p * 16 + (lane >> 2);
-        const int64_t m = rows + r;
-        const float* from = mine + r * kPad + (lane & 3) * 8;
-        const Vec<float, 4> g0 = load_vec<float, 4>(from), g1 = load_vec<float, 4>(from + 4), u0 = load_vec<float, 4>(from + 32), u1 = load_vec<float, 4>(from + 36);
-        if (m >= a.m.extent || f >= a.n_half) continue;
+    for (int p = 0; p < 32 / kRows; ++p) {
+      const int r = p * kRows + lane / kLanes;
+      const int64_t m = rows + r;
+      const float* from = mine + r * kPad + lane % kLanes * 8;
+      const Vec<float, 4> x0 = load_vec<float, 4>(from), x1 = load_vec<float, 4>(from + 4);
+      if constexpr (kHalves) {
+        const Vec<float, 4> u0 = load_vec<float, 4>(from + kColumns), u1 = load_vec<float, 4>(from + kColumns + 4);
+        if (m >= a.m.extent || n >= a.n_half) continue;
         Vec<T, 8> h, g, u;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float gate = e < 4 ? g0.at[e] : g1.at[e - 4], up = e < 4 ? u0.at[e] : u1.at[e - 4];
+          const float gate = e < 4 ? x0.at[e] : x1.at[e - 4], up = e < 4 ? u0.at[e] : u1.at[e - 4];
           h.at[e] = (T)(activate(a.act, gate) * up);
           g.at[e] = (T)gate;
           u.at[e] = (T)up;
         }
-        store_vec<T, 8>(static_cast<T*>(a.out) + m * a.out_stride + f, h);
+        store_vec<T, 8>(static_cast<T*>(a.out) + m * a.out_stride + n, h);
         if (a.pre) {
-          T* pre = static_cast<T*>(a.pre) + m * 2 * a.n_half + f;
+          T* pre = static_cast<T*>(a.pre) + m * 2 * a.n_half + n;
           store_vec<T, 8>(pre, g);
           store_vec<T, 8>(pre + a.n_half, u);
         }
-      }
-    } else {
-      const int64_t n = n0 + wave_n * 64 + (lane & 7) * 8;
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const int r = p * 8 + (lane >> 3);
-        const int64_t m = rows + r;
-        const float* from = mine + r * kPad + (lane & 7) * 8;
-        const Vec<float, 4> x0 = load_vec<float, 4>(from), x1 = load_vec<float, 4>(from + 4);
+      } else {
         if (m >= a.m.extent || n >= a.n.extent) continue;
         put_columns<T, EPILOGUE, O>(a, m, n, {x0.at[0], x0.at[1], x0.at[2], x0.at[3], x1.at[0], x1.at[1], x1.at[2], x1.at[3]});
       }
@@ -455,17 +469,17 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(O* out, int64_t stride, 
 template <typename T, int LM, int LN, int EPILOGUE, typename O>
 int gemm(Gemm a, hipStream_t stream) {
   const int64_t columns = EPILOGUE == kGated ? 2 * a.n_half : a.n.extent;
-  auto go = [&](auto size) {
-    constexpr int B = decltype(size)::value;
+  auto go = [&](auto size, auto waves_m, auto waves_n) {
+    constexpr int B = decltype(size)::value, WM = decltype(waves_m)::value, WN = decltype(waves_n)::value;
     const int64_t tm = ceil_div(a.m.extent, B), tn = ceil_div(columns, B);
     if (tm * tn > 0x7fffffff) return (int)FPSCHED_EINVAL;
     a.tiles_m = (int)tm;
     a.tiles_n = (int)tn;
-    gemm_kernel<T, LM, LN, EPILOGUE, O, B, B><<<dim3((unsigned)(tm * tn)), dim3(B * 2), 0, stream>>>(a);
+    gemm_kernel<T, LM, LN, EPILOGUE, O, B, B, WM, WN><<<dim3((unsigned)(tm * tn)), dim3(WM * WN * 64), 0, stream>>>(a);
     return launched();
   };
-  if (ceil_div(a.m.extent, 256) * ceil_div(columns, 256) >= 160) return go(std::integral_constant<int, 256>());
-  return go(std::integral_constant<int, 128>());
+  if (ceil_div(a.m.extent, 256) * ceil_div(columns, 256) >= 160) return go(std::integral_constant<int, 256>(), std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
+  return go(std::integral_constant<int, 128>(), std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
 }
 
 constexpr int64_t kMostStride = 1 << 21;   // (256 rows of a tile are within 2^31 bytes)
