@@ -13,6 +13,8 @@
 // The N operand is the matrix instruction's first, so that a lane holds four neighbouring n of one m, which is how rows are written.
 #include "ops_common.h"
 
+#include <algorithm>
+
 namespace fpsched {
 namespace {
 
@@ -34,7 +36,7 @@ struct Frag<_Float16> {
 };
 
 enum { kAlong, kDown };                        // how k lies in an operand
-enum { kStore, kGated, kGatedGrad };           // what becomes of a tile
+enum { kStore, kGated, kGatedGrad, kPart };    // what becomes of a tile
 constexpr int kDepth = 64;                     // k of a tile in LDS
 constexpr unsigned kOutside = 0x80000000u;     // an offset behind the end of every tile's buffer
 
@@ -54,6 +56,7 @@ struct Gemm {
   int act;
   void* pre;                 // kGated: written unless NULL; kGatedGrad: read
   int tiles_m, tiles_n;
+  int64_t part_depth;        // kPart: a part's k
 };
 
 // ---- activations: the value, and with it the derivative ----------------------------------------------------------------
@@ -180,7 +183,25 @@ __device__ __forceinline__ void tile_of(unsigned id, int tiles_m, int tiles_n, i
   *tn = in / high;
 }
 
-// What becomes of 8 neighbouring columns of a row.
+// What becomes of 8 neighbouring columns of a row, of the gate's half and the other one.
+template <typename T>
+__device__ __forceinline__ void put_gated(const Gemm& a, int64_t m, int64_t n, const Vec<float, 8>& gate, const Vec<float, 8>& up) {
+  Vec<T, 8> h, g, u;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    h.at[e] = (T)(activate(a.act, gate.at[e]) * up.at[e]);
+    g.at[e] = (T)gate.at[e];
+    u.at[e] = (T)up.at[e];
+  }
+  store_vec<T, 8>(static_cast<T*>(a.out) + m * a.out_stride + n, h);
+  if (a.pre) {
+    T* pre = static_cast<T*>(a.pre) + m * 2 * a.n_half + n;
+    store_vec<T, 8>(pre, g);
+    store_vec<T, 8>(pre + a.n_half, u);
+  }
+}
+
+// ... of 8 neighbouring columns of a row where there are no halves.
 template <typename T, int EPILOGUE, typename O>
 __device__ __forceinline__ void put_columns(const Gemm& a, int64_t m, int64_t n, const Vec<float, 8>& x) {
   if constexpr (EPILOGUE == kGatedGrad) {
@@ -235,6 +256,13 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
   const int wave_m = wave / kWavesN, wave_n = wave % kWavesN;
   int tm, tn;
   tile_of(blockIdx.x, a.tiles_m, a.tiles_n, &tm, &tn);
+  if constexpr (EPILOGUE == kPart) {   // blockIdx.y: a part of k, whose sums have a place of their own
+    const int64_t k0 = (int64_t)blockIdx.y * a.part_depth;
+    a.m.data = static_cast<const T*>(a.m.data) + k0 * (LM == kAlong ? 1 : a.m.stride);
+    a.n.data = static_cast<const T*>(a.n.data) + k0 * (LN == kAlong ? 1 : a.n.stride);
+    a.depth = min(a.part_depth, a.depth - k0);
+    a.out = static_cast<float*>(a.out) + blockIdx.y * a.m.extent * a.out_stride;
+  }
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * (kHalves ? BN / 2 : BN);
   f32x16 acc[MF][NF] = {};
   const int tiles = (int)((a.depth + kDepth - 1) / kDepth);
@@ -316,20 +344,8 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
       if constexpr (kHalves) {
         const Vec<float, 4> u0 = load_vec<float, 4>(from + kColumns), u1 = load_vec<float, 4>(from + kColumns + 4);
         if (m >= a.m.extent || n >= a.n_half) continue;
-        Vec<T, 8> h, g, u;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float gate = e < 4 ? x0.at[e] : x1.at[e - 4], up = e < 4 ? u0.at[e] : u1.at[e - 4];
-          h.at[e] = (T)(activate(a.act, gate) * up);
-          g.at[e] = (T)gate;
-          u.at[e] = (T)up;
-        }
-        store_vec<T, 8>(static_cast<T*>(a.out) + m * a.out_stride + n, h);
-        if (a.pre) {
-          T* pre = static_cast<T*>(a.pre) + m * 2 * a.n_half + n;
-          store_vec<T, 8>(pre, g);
-          store_vec<T, 8>(pre + a.n_half, u);
-        }
+        put_gated<T>(a, m, n, {x0.at[0], x0.at[1], x0.at[2], x0.at[3], x1.at[0], x1.at[1], x1.at[2], x1.at[3]},
+                     {u0.at[0], u0.at[1], u0.at[2], u0.at[3], u1.at[0], u1.at[1], u1.at[2], u1.at[3]});
       } else {
         if (m >= a.m.extent || n >= a.n.extent) continue;
         put_columns<T, EPILOGUE, O>(a, m, n, {x0.at[0], x0.at[1], x0.at[2], x0.at[3], x1.at[0], x1.at[1], x1.at[2], x1.at[3]});
@@ -465,21 +481,81 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(O* out, int64_t stride, 
     out[i / columns * stride + i % columns] = (O)0.f;
 }
 
-// Tiles of 256 x 256 where there are enough of them to go round the compute units, else of 128 x 128.
-template <typename T, int LM, int LN, int EPILOGUE, typename O>
-int gemm(Gemm a, hipStream_t stream) {
-  const int64_t columns = EPILOGUE == kGated ? 2 * a.n_half : a.n.extent;
-  auto go = [&](auto size, auto waves_m, auto waves_n) {
-    constexpr int B = decltype(size)::value, WM = decltype(waves_m)::value, WN = decltype(waves_n)::value;
-    const int64_t tm = ceil_div(a.m.extent, B), tn = ceil_div(columns, B);
-    if (tm * tn > 0x7fffffff) return (int)FPSCHED_EINVAL;
-    a.tiles_m = (int)tm;
-    a.tiles_n = (int)tn;
-    gemm_kernel<T, LM, LN, EPILOGUE, O, B, B, WM, WN><<<dim3((unsigned)(tm * tn)), dim3(WM * WN * 64), 0, stream>>>(a);
-    return launched();
+// The parts of a product added up in order, and what becomes of it.
+template <typename T, int EPILOGUE, typename O>
+__global__ __launch_bounds__(256) void add_parts_kernel(Gemm a, const float* parts, int n_parts) {
+  const int64_t columns = a.n.extent, pieces = (EPILOGUE == kGated ? a.n_half : columns) / 8;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, m = at / pieces, n = at % pieces * 8;
+  if (m >= a.m.extent) return;
+  auto total = [&](int64_t from) {
+    Vec<float, 8> sum = {};
+    for (int p = 0; p < n_parts; ++p) {
+      const float* x = parts + (p * a.m.extent + m) * columns + from;
+      const Vec<float, 4> low = load_vec<float, 4>(x), high = load_vec<float, 4>(x + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum.at[e] += low.at[e], sum.at[e + 4] += high.at[e];
+    }
+    return sum;
   };
-  if (ceil_div(a.m.extent, 256) * ceil_div(columns, 256) >= 160) return go(std::integral_constant<int, 256>(), std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
-  return go(std::integral_constant<int, 128>(), std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
+  if constexpr (EPILOGUE == kGated) put_gated<T>(a, m, n, total(n), total(a.n_half + n));
+  else put_columns<T, EPILOGUE, O>(a, m, n, total(n));
+}
+
+// How a product is cut.  Tiles of 256 x 256 where there are enough of them to go round the compute units, else of 128 x 128, two workgroups
+// to a compute unit; where even of those there are few, k is cut into parts, whose sums are added up by another kernel.  What decides is an
+// estimate: a tile's step of 64 k takes 0.65 us with one workgroup to a compute unit and 1.1 with two; the parts are
+// written and read at 8 TB/s, in a launch more.
+struct Split {
+  bool large;
+  int parts;
+  int64_t part_depth;
+};
+
+Split split(int64_t m, int64_t n, int64_t depth) {
+  Split s{ceil_div(m, 256) * ceil_div(n, 256) >= 160, 1, depth};
+  if (s.large) return s;
+  const int64_t tiles = ceil_div(m, 128) * ceil_div(n, 128), steps = ceil_div(depth, kDepth);
+  double best = 0;
+  for (int parts = 1; parts <= 16 && steps >= 4 * parts; ++parts) {
+    const int64_t each = ceil_div(steps, parts), groups = tiles * parts;
+    const double us = each * (groups <= 256 ? 0.65 : 1.1 * ceil_div(groups, 512)) + (parts > 1 ? 4 + parts * (m * n * 8 / 8e6) : 0);
+    if (parts == 1 || us < best) {
+      best = us;
+      s.parts = (int)ceil_div(steps, each);
+      s.part_depth = s.parts == 1 ? depth : each * kDepth;
+    }
+  }
+  return s;
+}
+
+size_t split_bytes(int64_t m, int64_t n, int64_t depth) {
+  const Split s = split(m, n, depth);
+  return s.parts > 1 ? (size_t)s.parts * m * n * sizeof(float) : 0;
+}
+
+template <typename T, int LM, int LN, int EPILOGUE, typename O>
+int gemm(Gemm a, void* workspace, hipStream_t stream) {
+  const int64_t columns = a.n.extent;   // (of kGated: both halves)
+  const Split s = split(a.m.extent, columns, a.depth);
+  const int64_t side = s.large ? 256 : 128, tm = ceil_div(a.m.extent, side), tn = ceil_div(columns, side);
+  if (tm * tn > 0x7fffffff) return FPSCHED_EINVAL;
+  a.tiles_m = (int)tm;
+  a.tiles_n = (int)tn;
+  if (s.large) {
+    gemm_kernel<T, LM, LN, EPILOGUE, O, 256, 256, 2, 4><<<dim3((unsigned)(tm * tn)), dim3(512), 0, stream>>>(a);
+  } else if (s.parts == 1) {
+    gemm_kernel<T, LM, LN, EPILOGUE, O, 128, 128, 2, 2><<<dim3((unsigned)(tm * tn)), dim3(256), 0, stream>>>(a);
+  } else {
+    Gemm part = a;
+    part.out = workspace;
+    part.out_stride = columns;
+    part.part_depth = s.part_depth;
+    part.accumulate = 0;
+    gemm_kernel<T, LM, LN, kPart, float, 128, 128, 2, 2><<<dim3((unsigned)(tm * tn), s.parts), dim3(256), 0, stream>>>(part);
+    const int64_t pieces = a.m.extent * ((EPILOGUE == kGated ? a.n_half : columns) / 8);
+    add_parts_kernel<T, EPILOGUE, O><<<dim3((unsigned)ceil_div(pieces, 256)), dim3(256), 0, stream>>>(a, static_cast<const float*>(workspace), s.parts);
+  }
+  return launched();
 }
 
 constexpr int64_t kMostStride = 1 << 21;   // (256 rows of a tile are within 2^31 bytes)
@@ -491,6 +567,20 @@ int check_sizes(int type, int act, int64_t n_tokens, int64_t width, int64_t hidd
   if (act < FPSCHED_SILU || act > FPSCHED_RELU || n_tokens < 0 || n_tokens > 0x7fffffffll) return FPSCHED_EINVAL;
   if (width < 8 || hidden_width < 8 || width % 8 || hidden_width % 8 || width > kMostStride || hidden_width > kMostStride / 2) return FPSCHED_EINVAL;
   return FPSCHED_OK;
+}
+
+// Room for the largest of the products' parts.
+size_t workspace_for(int64_t t, int64_t k, int64_t f) {
+  if (t == 0) return 16;
+  const size_t forward = t <= kFewRows ? 0 : std::max(split_bytes(t, 2 * f, k), split_bytes(t, k, f));
+  const size_t backward = std::max(split_bytes(t, f, k), split_bytes(t, k, 2 * f)), weights = std::max(split_bytes(2 * f, k, t), split_bytes(k, f, t));
+  return std::max<size_t>({16, forward, backward, weights});
+}
+
+int check_workspace(const void* workspace, size_t bytes, int64_t t, int64_t k, int64_t f) {
+  const size_t needed = workspace_for(t, k, f);
+  if (needed > 16 && (!workspace || !aligned(workspace, 16))) return FPSCHED_EINVAL;
+  return needed > 16 && bytes < needed ? FPSCHED_ENOMEM : FPSCHED_OK;
 }
 
 template <typename F>
@@ -507,7 +597,7 @@ extern "C" {
 
 size_t fpsched_op_ffn_workspace_bytes(int64_t n_tokens, int64_t width, int64_t hidden_width) {
   if (check_sizes(FPSCHED_BF16, 0, n_tokens, width, hidden_width) != FPSCHED_OK) return 0;
-  return 16;
+  return workspace_for(n_tokens, width, hidden_width);
 }
 
 int fpsched_op_ffn(int device_id, int type, int act, int64_t n_tokens, int64_t width, int64_t hidden_width, const void* x,
@@ -518,6 +608,8 @@ int fpsched_op_ffn(int device_id, int type, int act, int64_t n_tokens, int64_t w
   if (n_tokens == 0) return FPSCHED_OK;
   if (!row_ok(x, x_stride) || !row_ok(out, out_stride) || !row_ok(w_in, 0) || !row_ok(w_out, 0) || !row_ok(hidden, 0) || (pre && !aligned(pre, 16)))
     return FPSCHED_EINVAL;
+  const int room = check_workspace(d_workspace, workspace_bytes, n_tokens, width, hidden_width);
+  if (room != FPSCHED_OK) return room;
   OpsDevice g(device_id);
   if (!g.ok) return FPSCHED_EHIP;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -526,12 +618,12 @@ int fpsched_op_ffn(int device_id, int type, int act, int64_t n_tokens, int64_t w
     Gemm a = {};
     a.m = {x, x_stride, n_tokens}; a.n = {w_in, width, 2 * hidden_width}; a.depth = width; a.n_half = hidden_width;
     a.out = hidden; a.out_stride = hidden_width; a.act = act; a.pre = pre;
-    const int first = n_tokens <= kFewRows ? few_rows<T, kGated>(a, stream) : gemm<T, kAlong, kAlong, kGated, T>(a, stream);
+    const int first = n_tokens <= kFewRows ? few_rows<T, kGated>(a, stream) : gemm<T, kAlong, kAlong, kGated, T>(a, d_workspace, stream);
     if (first != FPSCHED_OK) return first;
     Gemm b = {};
     b.m = {hidden, hidden_width, n_tokens}; b.n = {w_out, hidden_width, width}; b.depth = hidden_width;
     b.out = out; b.out_stride = out_stride;
-    return n_tokens <= kFewRows ? few_rows<T, kStore>(b, stream) : gemm<T, kAlong, kAlong, kStore, T>(b, stream);
+    return n_tokens <= kFewRows ? few_rows<T, kStore>(b, stream) : gemm<T, kAlong, kAlong, kStore, T>(b, d_workspace, stream);
   });
 }
 
@@ -543,6 +635,8 @@ int fpsched_op_ffn_input_grad(int device_id, int type, int act, int64_t n_tokens
   if (n_tokens == 0) return FPSCHED_OK;
   if (!row_ok(grad, grad_stride) || !row_ok(d_x, d_x_stride) || !row_ok(w_in, 0) || !row_ok(w_out, 0) || !row_ok(pre, 0) || !row_ok(d_pre, 0))
     return FPSCHED_EINVAL;
+  const int room = check_workspace(d_workspace, workspace_bytes, n_tokens, width, hidden_width);
+  if (room != FPSCHED_OK) return room;
   OpsDevice g(device_id);
   if (!g.ok) return FPSCHED_EHIP;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -551,12 +645,12 @@ int fpsched_op_ffn_input_grad(int device_id, int type, int act, int64_t n_tokens
     Gemm a = {};
     a.m = {grad, grad_stride, n_tokens}; a.n = {w_out, hidden_width, hidden_width}; a.depth = width; a.n_half = hidden_width;
     a.out = d_pre; a.out_stride = 2 * hidden_width; a.act = act; a.pre = const_cast<void*>(pre);
-    const int first = gemm<T, kAlong, kDown, kGatedGrad, T>(a, stream);
+    const int first = gemm<T, kAlong, kDown, kGatedGrad, T>(a, d_workspace, stream);
     if (first != FPSCHED_OK) return first;
     Gemm b = {};
     b.m = {d_pre, 2 * hidden_width, n_tokens}; b.n = {w_in, width, width}; b.depth = 2 * hidden_width;
     b.out = d_x; b.out_stride = d_x_stride;
-    return gemm<T, kAlong, kDown, kStore, T>(b, stream);
+    return gemm<T, kAlong, kDown, kStore, T>(b, d_workspace, stream);
   });
 }
 
@@ -570,6 +664,8 @@ int fpsched_op_ffn_weight_grad(int device_id, int type, int64_t n_tokens, int64_
   if (!row_ok(d_w_in, 0) || !row_ok(d_w_out, 0)) return FPSCHED_EINVAL;
   if (n_tokens > 0 && (!row_ok(x, x_stride) || !row_ok(grad, grad_stride) || !row_ok(hidden, 0) || !row_ok(d_pre, 0))) return FPSCHED_EINVAL;
   if (n_tokens == 0 && accumulate) return FPSCHED_OK;
+  const int room = check_workspace(d_workspace, workspace_bytes, n_tokens, width, hidden_width);
+  if (room != FPSCHED_OK) return room;
   OpsDevice g(device_id);
   if (!g.ok) return FPSCHED_EHIP;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -585,12 +681,12 @@ int fpsched_op_ffn_weight_grad(int device_id, int type, int64_t n_tokens, int64_
       Gemm a = {};
       a.m = {d_pre, 2 * hidden_width, 2 * hidden_width}; a.n = {x, x_stride, width}; a.depth = n_tokens;
       a.out = d_w_in; a.out_stride = width; a.accumulate = accumulate;
-      const int first = gemm<T, kDown, kDown, kStore, O>(a, stream);
+      const int first = gemm<T, kDown, kDown, kStore, O>(a, d_workspace, stream);
       if (first != FPSCHED_OK) return first;
       Gemm b = {};
       b.m = {grad, grad_stride, width}; b.n = {hidden, hidden_width, hidden_width}; b.depth = n_tokens;
       b.out = d_w_out; b.out_stride = hidden_width; b.accumulate = accumulate;
-      return gemm<T, kDown, kDown, kStore, O>(b, stream);
+      return gemm<T, kDown, kDown, kStore, O>(b, d_workspace, stream);
     };
     if (out_type == FPSCHED_F32) return go(float());
     return go(T());
