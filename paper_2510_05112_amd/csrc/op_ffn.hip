@@ -357,10 +357,11 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
 
 // ---- few tokens --------------------------------------------------------------------------------------------------------
 //
-// At most kFewRows rows: the weights are read once, and that is what it takes.  A workgroup has 16 columns (16 of the gate's and the same of the
+// At most 16 rows: the weights are read once, and that is what it takes.  A workgroup has 16 columns (16 of the gate's and the same of the
 // other half's), its wavefronts a share of k each; weights go from memory to the matrix instruction's registers, 128 bytes of
-// a row at a time by four lanes, and the rows of x beside them from cache in the same order of k.
-constexpr int kFewRows = 64;
+// a row at a time by four lanes, and the rows of x beside them from cache in the same order of k.  (More rows, in sixteens: 17 to 64 of
+// 4,096 took 62 to 126 us, and the tiles with k in parts take 56 to 65.)
+constexpr int kFewRows = 16;
 
 template <typename T>
 struct Frag16;
@@ -374,30 +375,25 @@ struct Frag16<_Float16> {
   static __device__ __forceinline__ f32x4 mul(Frag<_Float16>::type a, Frag<_Float16>::type b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
-// MF: sixteens of rows.  SETS: 2 for kGated.
-template <typename T, int EPILOGUE, int MF, int WAVES>
+template <typename T, int EPILOGUE, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(Gemm a) {
   constexpr int kSets = EPILOGUE == kGated ? 2 : 1;
   using F = typename Frag<T>::type;
-  __shared__ __align__(16) float sums[WAVES][kSets * MF][64][4];
+  __shared__ __align__(16) float sums[WAVES][kSets][64][4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t n0 = (int64_t)blockIdx.x * 16;
   const int64_t columns = EPILOGUE == kGated ? a.n_half : a.n.extent;
   const int at = lane & 15, group = lane >> 4;
   const T* weights[kSets];
 #pragma unroll
-  for (int s = 0; s < kSets; ++s)
-    weights[s] = static_cast<const T*>(a.n.data) + (min(n0 + at, columns - 1) + s * a.n_half) * a.n.stride;
-  const T* rows[MF];
-#pragma unroll
-  for (int i = 0; i < MF; ++i) rows[i] = static_cast<const T*>(a.m.data) + min((int64_t)(i * 16 + at), a.m.extent - 1) * a.m.stride;
-  f32x4 acc[kSets][MF] = {};
-  constexpr int kPiece = 64;   // k that the four groups of lanes have together
-  const int64_t share = ((a.depth + kPiece * WAVES - 1) / (kPiece * WAVES)) * kPiece;
+  for (int s = 0; s < kSets; ++s) weights[s] = static_cast<const T*>(a.n.data) + (min(n0 + at, columns - 1) + s * a.n_half) * a.n.stride;
+  const T* row = static_cast<const T*>(a.m.data) + min((int64_t)at, a.m.extent - 1) * a.m.stride;
+  f32x4 acc[kSets] = {};
+  constexpr int kPiece = 64, kAhead = 4;   // k that the four groups of lanes have together; pieces on their way
+  const int64_t share = (a.depth + kPiece * WAVES - 1) / (kPiece * WAVES) * kPiece;
   const int64_t begin = wave * share, end = min(begin + share, a.depth);
-  constexpr int kAhead = MF == 1 ? 4 : 2;
   for (int64_t k0 = begin; k0 < end; k0 += kAhead * kPiece) {
-    F w[kAhead][kSets][2], x[kAhead][MF][2];
+    F w[kAhead][kSets][2], x[kAhead][2];
 #pragma unroll
     for (int p = 0; p < kAhead; ++p)
 #pragma unroll
@@ -410,67 +406,50 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(Gemm a) {
           w[p][s][j] = *reinterpret_cast<const F*>(weights[s] + from);
           if (!in) w[p][s][j] = F{};
         }
-#pragma unroll
-        for (int i = 0; i < MF; ++i) {
-          x[p][i][j] = *reinterpret_cast<const F*>(rows[i] + from);
-          if (!in) x[p][i][j] = F{};
-        }
+        x[p][j] = *reinterpret_cast<const F*>(row + from);
+        if (!in) x[p][j] = F{};
       }
 #pragma unroll
     for (int p = 0; p < kAhead; ++p)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int s = 0; s < kSets; ++s)
-#pragma unroll
-          for (int i = 0; i < MF; ++i) acc[s][i] = Frag16<T>::mul(w[p][s][j], x[p][i][j], acc[s][i]);
+        for (int s = 0; s < kSets; ++s) acc[s] = Frag16<T>::mul(w[p][s][j], x[p][j], acc[s]);
   }
+#pragma unroll
+  for (int s = 0; s < kSets; ++s) *reinterpret_cast<f32x4*>(sums[wave][s][lane]) = acc[s];
+  __syncthreads();
+  // four columns of a row a lane
+  const int64_t m = at, n = n0 + group * 4;
+  if (wave || m >= a.m.extent || n >= columns) return;
+  f32x4 total[kSets] = {};
 #pragma unroll
   for (int s = 0; s < kSets; ++s)
 #pragma unroll
-    for (int i = 0; i < MF; ++i) *reinterpret_cast<f32x4*>(sums[wave][s * MF + i][lane]) = acc[s][i];
-  __syncthreads();
-  // four columns of a row a thread: lane = row in its sixteen + 16 (columns / 4)
-  for (int v = threadIdx.x; v < MF * 64; v += WAVES * 64) {
-    const int i = v >> 6, l = v & 63;
-    const int64_t m = i * 16 + (l & 15), n = n0 + (l >> 4) * 4;
-    if (m >= a.m.extent || n >= columns) continue;
-    f32x4 total[kSets] = {};
+    for (int w = 0; w < WAVES; ++w) total[s] += *reinterpret_cast<const f32x4*>(sums[w][s][lane]);
+  if constexpr (EPILOGUE == kGated) {
+    Vec<T, 4> h, g, u;
 #pragma unroll
-    for (int s = 0; s < kSets; ++s)
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) total[s] += *reinterpret_cast<const f32x4*>(sums[w][s * MF + i][l]);
-    if constexpr (EPILOGUE == kGated) {
-      Vec<T, 4> h, g, u;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        h.at[e] = (T)(activate(a.act, total[0][e]) * total[1][e]);
-        g.at[e] = (T)total[0][e];
-        u.at[e] = (T)total[1][e];
-      }
-      store_vec<T, 4>(static_cast<T*>(a.out) + m * a.out_stride + n, h);
-      if (a.pre) {
-        T* pre = static_cast<T*>(a.pre) + m * 2 * a.n_half + n;
-        store_vec<T, 4>(pre, g);
-        store_vec<T, 4>(pre + a.n_half, u);
-      }
-    } else {
-      store_vec<T, 4>(static_cast<T*>(a.out) + m * a.out_stride + n, {(T)total[0][0], (T)total[0][1], (T)total[0][2], (T)total[0][3]});
+    for (int e = 0; e < 4; ++e) {
+      h.at[e] = (T)(activate(a.act, total[0][e]) * total[1][e]);
+      g.at[e] = (T)total[0][e];
+      u.at[e] = (T)total[1][e];
     }
+    store_vec<T, 4>(static_cast<T*>(a.out) + m * a.out_stride + n, h);
+    if (a.pre) {
+      T* pre = static_cast<T*>(a.pre) + m * 2 * a.n_half + n;
+      store_vec<T, 4>(pre, g);
+      store_vec<T, 4>(pre + a.n_half, u);
+    }
+  } else {
+    store_vec<T, 4>(static_cast<T*>(a.out) + m * a.out_stride + n, {(T)total[0][0], (T)total[0][1], (T)total[0][2], (T)total[0][3]});
   }
 }
 
 template <typename T, int EPILOGUE>
 int few_rows(const Gemm& a, hipStream_t stream) {
-  const int64_t columns = EPILOGUE == kGated ? a.n_half : a.n.extent;
-  const dim3 grid((unsigned)ceil_div(columns, 16));
   constexpr int W = EPILOGUE == kGated ? 4 : 8;   // (the second product has fewer columns and a longer k)
-  switch ((a.m.extent + 15) / 16) {
-    case 1: few_rows_kernel<T, EPILOGUE, 1, W><<<grid, dim3(W * 64), 0, stream>>>(a); break;
-    case 2: few_rows_kernel<T, EPILOGUE, 2, W><<<grid, dim3(W * 64), 0, stream>>>(a); break;
-    case 3: few_rows_kernel<T, EPILOGUE, 3, W><<<grid, dim3(W * 64), 0, stream>>>(a); break;
-    default: few_rows_kernel<T, EPILOGUE, 4, W><<<grid, dim3(W * 64), 0, stream>>>(a); break;
-  }
+  few_rows_kernel<T, EPILOGUE, W><<<dim3((unsigned)ceil_div(EPILOGUE == kGated ? a.n_half : a.n.extent, 16)), dim3(W * 64), 0, stream>>>(a);
   return launched();
 }
 
