@@ -5,11 +5,14 @@
 //
 // Gradient: dE[v] = scale sum over {t : tokens[t] = v} grad[t].  Adding rows with atomics would make the sums depend on
 // their order; here the occurrences are sorted by token (a stable counting sort, 8 bits of the token a pass), so that each row of
-// dE is the sum of a run of sorted occurrences, and every row is written once.  Text repeats its few commonest tokens thousands of times: so that a
-// run's length bounds nothing, the sorted occurrences are cut into blocks of 32 without regard to runs, each summed by
-// workgroups of its own; a run inside one block is written where it belongs, one across blocks leaves its part (32 bits) in the workspace, and the pass
-// that writes the rows without a token adds the parts up.  Floor: grad read once, dE written once.
+// dE is the sum of a run of sorted occurrences.  Text repeats its few commonest tokens thousands of times: so that a
+// run's length bounds nothing, the sorted occurrences are cut into blocks of 16 without regard to runs, each summed by
+// workgroups of its own; a run inside one block is written where it belongs, one across blocks leaves its parts (32 bits) in the workspace, which
+// another kernel adds up.  Most rows of a large vocabulary have no token: all are filled with zeros by what the sort leaves of the chip.
+// Floor: grad read once, dE written once.
 #include "ops_common.h"
+
+#include <algorithm>
 
 namespace fpsched {
 namespace {
@@ -45,14 +48,156 @@ __global__ __launch_bounds__(kThreads) void embedding_kernel(const T* table, int
   }
 }
 
+// ---- zeros -------------------------------------------------------------------------------------------------------------
+
+// A slice of the table's rows to be filled with zeros by the workgroups from `first` on (bytes of an element: 2 or 4).
+struct Fill {
+  char* out;              // NULL: nothing to fill
+  int64_t rows, row_bytes, stride_bytes;   // adjacent rows are one row
+  int wide;               // rows begin at multiples of 16 bytes
+  int element;
+  unsigned first;
+  int slice, slices;
+
+  __device__ __forceinline__ bool mine() const { return blockIdx.x >= first; }
+  __device__ void run() const {
+    if (!out) return;
+    const int64_t at = (int64_t)(blockIdx.x - first) * blockDim.x + threadIdx.x, all = (int64_t)(gridDim.x - first) * blockDim.x;
+    const int unit = wide ? 16 : element;
+    const int64_t units = row_bytes / unit;
+    auto put = [&](char* to) {
+      if (wide) *reinterpret_cast<Vec<unsigned, 4>*>(to) = {};
+      else if (element == 4) *reinterpret_cast<unsigned*>(to) = 0;
+      else *reinterpret_cast<unsigned short*>(to) = 0;
+    };
+    if (rows == 1) {
+      // (a workgroup's four stores are neighbours)
+      const int64_t end = units * (slice + 1) / slices;
+      for (int64_t i = units * slice / slices + (at - threadIdx.x) * 4 + threadIdx.x; i < end; i += all * 4)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (i + k * blockDim.x < end) put(out + (i + k * blockDim.x) * unit);
+    } else {
+      const int64_t end = rows * (slice + 1) / slices;
+      for (int64_t r = rows * slice / slices + blockIdx.x - first; r < end; r += gridDim.x - first)
+        for (int64_t i = threadIdx.x; i < units; i += blockDim.x) put(out + r * stride_bytes + i * unit);
+    }
+    // (what is left of rows that are no multiple of 16 bytes)
+    const int left = (int)(row_bytes % unit);
+    if (left && slice == slices - 1)
+      for (int64_t i = at; i < rows * left; i += all) out[i / left * stride_bytes + units * unit + i % left] = 0;
+  }
+};
+
 // ---- sorting the occurrences -------------------------------------------------------------------------------------------
 
-constexpr int kDigits = 256, kSortRounds = 8;
-constexpr int kSortTile = kThreads * kSortRounds;   // occurrences a workgroup places
+constexpr int kDigits = 256;
 
 struct Occurrence {
   unsigned token, at;
 };
+
+// The lanes with the same digit, among those that have one.
+__device__ __forceinline__ unsigned long long same_digit(bool have, unsigned digit) {
+  unsigned long long same = __ballot(have);
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    const unsigned long long ones = __ballot(have && (digit >> b & 1));
+    same &= digit >> b & 1 ? ones : ~ones;
+  }
+  return same;
+}
+__device__ __forceinline__ unsigned lanes_in_front(unsigned long long of, int lane) { return __popcll(of & ((1ull << lane) - 1)); }
+
+// Up to kOneSort occurrences, all passes by one workgroup in LDS.  A wavefront has 64 `rounds` adjacent ones; a lane's place among those
+// of its digit is counted wavefront by wavefront, then over the wavefronts, then over the digits.
+constexpr unsigned kNone = ~0u;   // (a table has fewer rows)
+constexpr int kOneRounds = 16, kOneSort = 1024 * kOneRounds;
+
+__global__ __launch_bounds__(1024) void sort_few_kernel(const void* tokens, int tokens64, int n_tokens, int64_t n_rows, Occurrence* sorted,
+                                                       unsigned* total, Fill fill) {
+  if (fill.mine()) return fill.run();
+  __shared__ unsigned held_token[kOneSort];
+  __shared__ unsigned short held_at[kOneSort];
+  __shared__ unsigned short next[16][kDigits];
+  __shared__ unsigned sums[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int rounds = (n_tokens + 1023) / 1024;
+  int n = n_tokens;
+  for (int shift = 0; shift == 0 || (n_rows - 1) >> shift != 0; shift += 8) {
+    unsigned token[kOneRounds];     // kNone: none
+    unsigned at_rank[kOneRounds];   // which occurrence it is; in the upper half, its place among those of its digit
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r) {
+      const int i = (wave * rounds + r) * 64 + lane;
+      token[r] = kNone, at_rank[r] = 0;
+      if (r < rounds && i < n) {
+        if (shift == 0) {
+          const int64_t t = token_at(tokens, tokens64, i);
+          if (t >= 0 && t < n_rows) token[r] = (unsigned)t, at_rank[r] = (unsigned)i;
+        } else {
+          token[r] = held_token[i], at_rank[r] = held_at[i];
+        }
+      }
+    }
+    for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) next[0][i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r) {
+      if (r < rounds) {
+        const bool have = token[r] != kNone;
+        const unsigned digit = token[r] >> shift & (kDigits - 1);
+        const unsigned long long same = same_digit(have, digit);
+        const unsigned ahead = lanes_in_front(same, lane);
+        unsigned base = 0;
+        if (have) base = next[wave][digit];
+        __builtin_amdgcn_wave_barrier();
+        if (have && ahead == 0) next[wave][digit] = (unsigned short)(base + __popcll(same));
+        __builtin_amdgcn_wave_barrier();
+        at_rank[r] |= (base + ahead) << 16;
+      }
+    }
+    __syncthreads();
+    unsigned mine = 0, before = 0;
+    if (threadIdx.x < kDigits) {
+#pragma unroll
+      for (int w = 0; w < 16; ++w) mine += next[w][threadIdx.x];
+      unsigned incl = mine;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const unsigned other = __shfl_up(incl, d);
+        incl += lane >= d ? other : 0u;
+      }
+      if (lane == 63) sums[wave] = incl;
+      before = incl - mine;
+    }
+    __syncthreads();
+    n = (int)(sums[0] + sums[1] + sums[2] + sums[3]);
+    if (threadIdx.x < kDigits) {
+      for (int w = 0; w < wave; ++w) before += sums[w];
+#pragma unroll
+      for (int w = 0; w < 16; ++w) {
+        const unsigned c = next[w][threadIdx.x];
+        next[w][threadIdx.x] = (unsigned short)before;
+        before += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r)
+      if (token[r] != kNone) {
+        const unsigned place = next[wave][token[r] >> shift & (kDigits - 1)] + (at_rank[r] >> 16);
+        held_token[place] = token[r];
+        held_at[place] = (unsigned short)at_rank[r];
+      }
+    __syncthreads();
+  }
+  for (int i = threadIdx.x; i < n; i += 1024) sorted[i] = {held_token[i], held_at[i]};
+  if (threadIdx.x == 0) *total = (unsigned)n;
+}
+
+// More of them: three kernels a pass, over tiles of kSortTile.
+constexpr int kSortRounds = 8, kSortTile = kThreads * kSortRounds;
 
 // An occurrence to be sorted: of the first pass from the tokens (those outside the table are none), later of the pass before
 // (`n` of them).
@@ -64,6 +209,7 @@ struct SortSource {
   const unsigned* n;
 
   __device__ __forceinline__ bool get(int64_t i, Occurrence* o) const {
+    o->token = o->at = 0;
     if (sorted) {
       if (i >= *n) return false;
       *o = sorted[i];
@@ -78,7 +224,8 @@ struct SortSource {
 };
 
 // counts[digit][workgroup]
-__global__ __launch_bounds__(kThreads) void sort_count_kernel(SortSource src, int shift, unsigned* counts) {
+__global__ __launch_bounds__(kThreads) void sort_count_kernel(SortSource src, int shift, unsigned* counts, Fill fill) {
+  if (fill.mine()) return fill.run();
   __shared__ unsigned held[kDigits];
   held[threadIdx.x] = 0;
   __syncthreads();
@@ -88,11 +235,12 @@ __global__ __launch_bounds__(kThreads) void sort_count_kernel(SortSource src, in
     if (src.get(first + r * kThreads + threadIdx.x, &o)) atomicAdd(&held[(o.token >> shift) & (kDigits - 1)], 1u);
   }
   __syncthreads();
-  counts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = held[threadIdx.x];
+  counts[(int64_t)threadIdx.x * fill.first + blockIdx.x] = held[threadIdx.x];
 }
 
 // counts -> the place of the first occurrence of each (digit, workgroup); *total: how many there are
-__global__ __launch_bounds__(1024) void sort_scan_kernel(unsigned* counts, int64_t n, unsigned* total) {
+__global__ __launch_bounds__(1024) void sort_scan_kernel(unsigned* counts, int64_t n, unsigned* total, Fill fill) {
+  if (fill.mine()) return fill.run();
   __shared__ unsigned waves[16];
   unsigned before = 0;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -130,9 +278,10 @@ __global__ __launch_bounds__(1024) void sort_scan_kernel(unsigned* counts, int64
   if (threadIdx.x == 0) *total = before;
 }
 
-// Places a workgroup's occurrences in order.  Each wavefront takes a piece of them, counts its digits first (lanes with one
-// digit find each other by eight ballots), and places them behind those of the wavefronts in front of it.
-__global__ __launch_bounds__(kThreads) void sort_place_kernel(SortSource src, int shift, const unsigned* places, Occurrence* out) {
+// Places a workgroup's occurrences in order.  Each wavefront takes a piece of them, counts its digits first, and places them behind
+// those of the wavefronts in front of it.
+__global__ __launch_bounds__(kThreads) void sort_place_kernel(SortSource src, int shift, const unsigned* places, Occurrence* out, Fill fill) {
+  if (fill.mine()) return fill.run();
   __shared__ unsigned next[kThreads / 64][kDigits];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int w = 0; w < kThreads / 64; ++w) next[w][threadIdx.x] = 0;
@@ -142,16 +291,12 @@ __global__ __launch_bounds__(kThreads) void sort_place_kernel(SortSource src, in
   unsigned rank[kSortRounds];
   bool have[kSortRounds];
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
-    have[r] = src.get(first + r * 64, &o[r]);
-    const unsigned digit = (o[r].token >> shift) & (kDigits - 1);
-    unsigned long long same = __ballot(have[r]);
+  for (int r = 0; r < kSortRounds; ++r) have[r] = src.get(first + r * 64, &o[r]);
 #pragma unroll
-    for (int b = 0; b < 8; ++b) {
-      const unsigned long long ones = __ballot(have[r] && (digit >> b & 1));
-      same &= digit >> b & 1 ? ones : ~ones;
-    }
-    const int ahead = __popcll(same & ((1ull << lane) - 1));
+  for (int r = 0; r < kSortRounds; ++r) {
+    const unsigned digit = (o[r].token >> shift) & (kDigits - 1);
+    const unsigned long long same = same_digit(have[r], digit);
+    const unsigned ahead = lanes_in_front(same, lane);
     unsigned base = 0;
     if (have[r]) base = next[wave][digit];
     __builtin_amdgcn_wave_barrier();
@@ -160,7 +305,7 @@ __global__ __launch_bounds__(kThreads) void sort_place_kernel(SortSource src, in
     rank[r] = base + ahead;
   }
   __syncthreads();
-  unsigned at = places[(int64_t)threadIdx.x * gridDim.x + blockIdx.x];
+  unsigned at = places[(int64_t)threadIdx.x * fill.first + blockIdx.x];
   for (int w = 0; w < kThreads / 64; ++w) {
     const unsigned c = next[w][threadIdx.x];
     next[w][threadIdx.x] = at;
@@ -172,21 +317,9 @@ __global__ __launch_bounds__(kThreads) void sort_place_kernel(SortSource src, in
     if (have[r]) out[next[wave][(o[r].token >> shift) & (kDigits - 1)] + rank[r]] = o[r];
 }
 
-// starts[v]: the first sorted occurrence of a token >= v
-__global__ __launch_bounds__(kThreads) void row_starts_kernel(const Occurrence* sorted, const unsigned* n, int64_t n_rows, unsigned* starts) {
-  const int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (v > n_rows) return;
-  unsigned low = 0, high = *n;
-  while (low < high) {
-    const unsigned mid = (low + high) >> 1;
-    if (sorted[mid].token < (unsigned)v) low = mid + 1; else high = mid;
-  }
-  starts[v] = low;
-}
-
 // ---- sums --------------------------------------------------------------------------------------------------------------
 
-constexpr int kBlock = 32;   // sorted occurrences that are summed in one go
+constexpr int kBlock = 16;   // sorted occurrences that are summed in one go
 
 template <typename O, int N>
 __device__ __forceinline__ void put_sum(O* out, const float* sum, float scale, int accumulate, int64_t c, int64_t width) {
@@ -206,37 +339,44 @@ __device__ __forceinline__ void put_sum(O* out, const float* sum, float scale, i
 // blockIdx.x: block of sorted occurrences, blockIdx.y: piece of the width.  Part 2 b: of the run that block b begins in
 // the middle of, 2 b + 1: of the run that goes on behind it.
 template <typename T, typename O, int N>
-__global__ __launch_bounds__(64) void row_sums_kernel(const T* grad, int64_t grad_stride, int64_t width, const Occurrence* sorted,
-                                                     const unsigned* n, const unsigned* starts, float scale, O* out, int64_t out_stride,
-                                                     int accumulate, float* parts, int64_t part_stride) {
+__global__ __launch_bounds__(64) void row_sums_kernel(const T* __restrict__ grad, int64_t grad_stride, int64_t width,
+                                                     const Occurrence* __restrict__ sorted, const unsigned* __restrict__ n, float scale,
+                                                     O* __restrict__ out, int64_t out_stride, int accumulate, float* __restrict__ parts,
+                                                     int64_t part_stride) {
   const unsigned first = blockIdx.x * (unsigned)kBlock, all = *n;
   if (first >= all) return;
   const unsigned end = min(first + kBlock, all);
-  const int64_t c = ((int64_t)blockIdx.y * 64 + threadIdx.x) * N;
-  if (c >= width) return;
+  // A lane an occurrence, for all lanes to read: lanes behind the width stay, with the first column's addresses, and write nothing (a lane that
+  // has returned loads nothing, and what others read of its registers is anything).
+  const Occurrence mine = sorted[min(first + threadIdx.x % kBlock, end - 1)];
+  const int64_t column = ((int64_t)blockIdx.y * 64 + threadIdx.x) * N;
+  const bool live = column < width;
+  const int64_t c = live ? column : 0;
   const bool whole = c + N <= width;
   float sum[N] = {};
-  auto flush = [&](unsigned token) {
-    const unsigned from = starts[token], to = starts[token + 1];
-    if (from >= first && to <= end) {
-      put_sum<O, N>(out + (int64_t)token * out_stride, sum, scale, accumulate, c, width);
+  unsigned now = sorted[first].token;
+  bool inside = first == 0 || sorted[first - 1].token != now;   // the run that is being summed begins in this block
+  const bool goes_on = end < all && sorted[end].token == sorted[end - 1].token;
+  auto flush = [&](bool ends) {
+    if (!live) {
+    } else if (inside && ends) {
+      put_sum<O, N>(out + (int64_t)now * out_stride, sum, scale, accumulate, c, width);
     } else {
-      float* part = parts + (2 * (int64_t)blockIdx.x + (from >= first)) * part_stride + c;   // (part_stride has room for whole vectors)
+      float* part = parts + (2 * (int64_t)blockIdx.x + inside) * part_stride + c;   // (part_stride has room for whole vectors)
 #pragma unroll
       for (int i = 0; i < N; ++i) part[i] = sum[i];
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] = 0.f;
   };
-  unsigned now = sorted[first].token;
   constexpr int kAhead = 8;
-  for (unsigned at = first; at < end; at += kAhead) {
-    Occurrence o[kAhead];
+  const int count = (int)(end - first);
+#pragma unroll 1
+  for (int b = 0; b < count; b += kAhead) {
     Vec<T, N> v[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      o[i] = sorted[min(at + i, end - 1)];
-      const T* from = grad + (int64_t)o[i].at * grad_stride + c;
+      const T* from = grad + (int64_t)__builtin_amdgcn_readlane(mine.at, b + i) * grad_stride + c;
       if (whole) {
         v[i] = load_vec<T, N>(from);
       } else {
@@ -248,41 +388,47 @@ __global__ __launch_bounds__(64) void row_sums_kernel(const T* grad, int64_t gra
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      if (at + i >= end) break;
-      if (o[i].token != now) {
-        flush(now);
-        now = o[i].token;
-      }
+      if (b + i < count) {
+        const unsigned token = __builtin_amdgcn_readlane(mine.token, b + i);
+        if (token != now) {
+          flush(true);
+          now = token;
+          inside = true;
+        }
 #pragma unroll
-      for (int e = 0; e < N; ++e) sum[e] += (float)v[i].at[e];
+        for (int e = 0; e < N; ++e) sum[e] += (float)v[i].at[e];
+      }
     }
   }
-  flush(now);
+  flush(!goes_on);
 }
 
-// The rows that no block wrote: without a token, or with a run across blocks, whose parts are added up.
+// The runs across blocks: the workgroups of the block that one begins in add up its parts.
 template <typename O, int N>
-__global__ __launch_bounds__(kThreads) void row_rest_kernel(const unsigned* starts, int64_t n_rows, int64_t width, const float* parts,
-                                                           int64_t part_stride, float scale, O* out, int64_t out_stride, int accumulate,
-                                                           int lanes_shift) {
-  const int64_t v = ((int64_t)blockIdx.x << (8 - lanes_shift)) + (threadIdx.x >> lanes_shift);
-  if (v >= n_rows) return;
-  const unsigned from = starts[v], to = starts[v + 1];
-  const int lanes = 1 << lanes_shift;
-  const bool none = from == to;
-  if (none ? accumulate != 0 : from / kBlock == (to - 1) / kBlock) return;
-  for (int64_t c = (int64_t)(threadIdx.x & (lanes - 1)) * N; c < width; c += (int64_t)lanes * N) {
-    float sum[N] = {};
-    if (!none) {
-      const unsigned b0 = from / kBlock, b1 = (to - 1) / kBlock;
-      for (unsigned b = b0; b <= b1; ++b) {
-        const float* part = parts + (2 * (int64_t)b + (b == b0)) * part_stride + c;
-#pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] += part[i];
-      }
-    }
-    put_sum<O, N>(out + v * out_stride, sum, scale, accumulate, c, width);
+__global__ __launch_bounds__(64) void join_runs_kernel(const Occurrence* __restrict__ sorted, const unsigned* __restrict__ n, int64_t width,
+                                                      const float* __restrict__ parts, int64_t part_stride, float scale,
+                                                      O* __restrict__ out, int64_t out_stride, int accumulate) {
+  const unsigned first = blockIdx.x * (unsigned)kBlock, all = *n, end = first + kBlock;
+  if (end >= all) return;
+  const unsigned token = sorted[end - 1].token;
+  if (sorted[end].token != token) return;
+  if (sorted[first].token == token && first > 0 && sorted[first - 1].token == token) return;   // (it begins further in front)
+  // the last block that has some of it (its tokens begin blocks up to there)
+  unsigned low = blockIdx.x + 1, high = (all - 1) / kBlock;
+  while (low < high) {
+    const unsigned mid = (low + high + 1) >> 1;
+    if (sorted[mid * kBlock].token == token) low = mid; else high = mid - 1;
   }
+  const int64_t c = ((int64_t)blockIdx.y * 64 + threadIdx.x) * N;
+  if (c >= width) return;
+  float sum[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum[i] = parts[(2 * (int64_t)blockIdx.x + 1) * part_stride + c + i];
+  for (unsigned b = blockIdx.x + 1; b <= low; ++b) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] += parts[2 * (int64_t)b * part_stride + c + i];
+  }
+  put_sum<O, N>(out + (int64_t)token * out_stride, sum, scale, accumulate, c, width);
 }
 
 // lanes for a row: the power of two of them, at most a workgroup's, that a row of `vectors` has work for
@@ -293,13 +439,13 @@ int row_lanes_shift(int64_t vectors) {
 }
 
 struct GradWorkspace {
-  size_t sorted[2], counts, starts, parts, total, bytes;
+  size_t sorted[2], counts, parts, total, bytes;
   int64_t part_stride, tiles, blocks;
 };
 
-GradWorkspace grad_workspace(int64_t n_rows, int64_t width, int64_t n_tokens) {
+GradWorkspace grad_workspace(int64_t width, int64_t n_tokens) {
   GradWorkspace w;
-  w.tiles = ceil_div(n_tokens, kSortTile);
+  w.tiles = std::max<int64_t>(1, ceil_div(n_tokens, kSortTile));
   w.blocks = ceil_div(n_tokens, kBlock);
   w.part_stride = (int64_t)round_up((size_t)width, 8);
   size_t at = 0;
@@ -307,7 +453,6 @@ GradWorkspace grad_workspace(int64_t n_rows, int64_t width, int64_t n_tokens) {
   for (size_t& s : w.sorted) s = take((size_t)n_tokens * sizeof(Occurrence));
   w.counts = take((size_t)w.tiles * kDigits * 4);
   w.total = take(4);
-  w.starts = take((size_t)(n_rows + 1) * 4);
   w.parts = take((size_t)w.blocks * 2 * w.part_stride * 4);
   w.bytes = at;
   return w;
@@ -346,7 +491,7 @@ int fpsched_op_embedding(int device_id, int type, const void* table, int64_t tab
 
 size_t fpsched_op_embedding_grad_workspace_bytes(int64_t n_rows, int64_t width, int64_t n_tokens) {
   if (n_rows < 0 || width < 0 || width > kMaxWidth || n_tokens < 0 || n_rows > 0x7ffffffell || n_tokens > 0x7fffffffll) return 0;
-  return grad_workspace(n_rows, width, n_tokens).bytes;
+  return grad_workspace(width, n_tokens).bytes;
 }
 
 int fpsched_op_embedding_grad(int device_id, int type, const void* grad, int64_t grad_stride, int64_t n_rows, int64_t width,
@@ -359,25 +504,55 @@ int fpsched_op_embedding_grad(int device_id, int type, const void* grad, int64_t
   if (device_id < 0) return FPSCHED_ENODEV;
   if (n_rows == 0 || width == 0) return FPSCHED_OK;
   if (!out || (n_tokens > 0 && (!grad || !tokens)) || !d_workspace || !aligned(d_workspace, 16)) return FPSCHED_EINVAL;
-  const GradWorkspace w = grad_workspace(n_rows, width, n_tokens);
+  const GradWorkspace w = grad_workspace(width, n_tokens);
   if (workspace_bytes < w.bytes) return FPSCHED_ENOMEM;
   OpsDevice g(device_id);
   if (!g.ok) return FPSCHED_EHIP;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   char* base = static_cast<char*>(d_workspace);
   unsigned *counts = reinterpret_cast<unsigned*>(base + w.counts), *total = reinterpret_cast<unsigned*>(base + w.total);
-  unsigned* starts = reinterpret_cast<unsigned*>(base + w.starts);
   float* parts = reinterpret_cast<float*>(base + w.parts);
-  SortSource src{tokens, tokens64, n_tokens, n_rows, nullptr, total};
-  int which = 0;
-  for (int shift = 0; shift == 0 || (n_rows - 1) >> shift != 0; shift += 8, which ^= 1) {
-    if (w.tiles) sort_count_kernel<<<dim3((unsigned)w.tiles), dim3(kThreads), 0, stream>>>(src, shift, counts);
-    sort_scan_kernel<<<dim3(1), dim3(1024), 0, stream>>>(counts, w.tiles * kDigits, total);
-    Occurrence* placed = reinterpret_cast<Occurrence*>(base + w.sorted[which]);
-    if (w.tiles) sort_place_kernel<<<dim3((unsigned)w.tiles), dim3(kThreads), 0, stream>>>(src, shift, counts, placed);
-    src.sorted = placed;
+  // zeros everywhere, in slices beside the kernels that sort
+  const int out_size = out_type == FPSCHED_F32 ? 4 : 2;
+  Fill fill = {};
+  if (!accumulate) {
+    fill.out = static_cast<char*>(out);
+    const bool adjacent = out_stride == width || n_rows == 1;
+    fill.rows = adjacent ? 1 : n_rows;
+    fill.row_bytes = (adjacent ? n_rows : 1) * width * out_size;
+    fill.stride_bytes = out_stride * out_size;
+    fill.wide = aligned(out, 16) && (adjacent || out_stride * out_size % 16 == 0);
+    fill.element = out_size;
   }
-  row_starts_kernel<<<dim3((unsigned)ceil_div(n_rows + 1, kThreads)), dim3(kThreads), 0, stream>>>(src.sorted, total, n_rows, starts);
+  auto grid = [&](int64_t groups, int threads) {   // the kernel's own workgroups and those that fill
+    fill.first = (unsigned)groups;
+    const int64_t fillers = !fill.out ? 0 : std::min<int64_t>(2048 * 256 / threads, ceil_div(fill.rows * ceil_div(fill.row_bytes, 16), (int64_t)threads * 4 * fill.slices) + 1);
+    return dim3((unsigned)(groups + fillers));
+  };
+  const Occurrence* sorted = reinterpret_cast<const Occurrence*>(base + w.sorted[0]);
+  if (n_tokens <= kOneSort) {
+    fill.slices = 1;
+    const dim3 groups = grid(1, 1024);
+    sort_few_kernel<<<groups, dim3(1024), 0, stream>>>(tokens, tokens64, (int)n_tokens, n_rows, reinterpret_cast<Occurrence*>(base + w.sorted[0]), total, fill);
+  } else {
+    int passes = 1;
+    while ((n_rows - 1) >> 8 * passes) ++passes;
+    fill.slices = 3 * passes;
+    SortSource src{tokens, tokens64, n_tokens, n_rows, nullptr, total};
+    for (int pass = 0; pass < passes; ++pass) {
+      Occurrence* placed = reinterpret_cast<Occurrence*>(base + w.sorted[pass & 1]);
+      const dim3 many = grid(w.tiles, kThreads);
+      sort_count_kernel<<<many, dim3(kThreads), 0, stream>>>(src, 8 * pass, counts, fill);
+      ++fill.slice;
+      const dim3 one = grid(1, 1024);
+      sort_scan_kernel<<<one, dim3(1024), 0, stream>>>(counts, w.tiles * kDigits, total, fill);
+      ++fill.slice;
+      fill.first = (unsigned)w.tiles;
+      sort_place_kernel<<<many, dim3(kThreads), 0, stream>>>(src, 8 * pass, counts, placed, fill);
+      ++fill.slice;
+      src.sorted = sorted = placed;
+    }
+  }
   return with_type(type, [&](auto zero) {
     using T = decltype(zero);
     return with_type(out_type, [&](auto zero_out) {
@@ -387,13 +562,12 @@ int fpsched_op_embedding_grad(int device_id, int type, const void* grad, int64_t
       } else {
         auto go = [&](auto n) {
           constexpr int N = decltype(n)::value;
-          if (w.blocks)
-            row_sums_kernel<T, O, N><<<dim3((unsigned)w.blocks, (unsigned)ceil_div(width, 64 * N)), dim3(64), 0, stream>>>(
-                static_cast<const T*>(grad), grad_stride, width, src.sorted, total, starts, scale, static_cast<O*>(out), out_stride, accumulate,
-                parts, w.part_stride);
-          const int shift = row_lanes_shift(ceil_div(width, N));
-          row_rest_kernel<O, N><<<dim3((unsigned)ceil_div(n_rows, kThreads >> shift)), dim3(kThreads), 0, stream>>>(
-              starts, n_rows, width, parts, w.part_stride, scale, static_cast<O*>(out), out_stride, accumulate, shift);
+          if (w.blocks) {
+            const dim3 blocks((unsigned)w.blocks, (unsigned)ceil_div(width, 64 * N));
+            row_sums_kernel<T, O, N><<<blocks, dim3(64), 0, stream>>>(static_cast<const T*>(grad), grad_stride, width, sorted, total, scale,
+                                                                      static_cast<O*>(out), out_stride, accumulate, parts, w.part_stride);
+            join_runs_kernel<O, N><<<blocks, dim3(64), 0, stream>>>(sorted, total, width, parts, w.part_stride, scale, static_cast<O*>(out), out_stride, accumulate);
+          }
           return launched();
         };
         // (16 bytes of the gradient a lane, and as many elements of the output: of 32 bits two pieces of 16 bytes)
