@@ -424,10 +424,23 @@ __global__ __launch_bounds__(64) void join_runs_kernel(const Occurrence* __restr
   float sum[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) sum[i] = parts[(2 * (int64_t)blockIdx.x + 1) * part_stride + c + i];
-  for (unsigned b = blockIdx.x + 1; b <= low; ++b) {
+  const float* from = parts + 2 * (int64_t)(blockIdx.x + 1) * part_stride + c;
+  constexpr unsigned kAhead = 8;
+  unsigned b = blockIdx.x + 1;
+  for (; b + kAhead <= low + 1; b += kAhead) {
+    float x[kAhead][N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum[i] += parts[2 * (int64_t)b * part_stride + c + i];
+    for (unsigned j = 0; j < kAhead; ++j, from += 2 * part_stride)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[j][i] = from[i];
+#pragma unroll
+    for (unsigned j = 0; j < kAhead; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] += x[j][i];
   }
+  for (; b <= low; ++b, from += 2 * part_stride)
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] += from[i];
   put_sum<O, N>(out + (int64_t)token * out_stride, sum, scale, accumulate, c, width);
 }
 

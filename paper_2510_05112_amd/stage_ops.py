@@ -56,33 +56,39 @@ def _lib():
 
 
 # ---- arguments -------------------------------------------------------------------------------------------------------
+# (messages are put together only where they are raised: a call's checks take as long as its launch otherwise)
 
-def _types():
-    import torch
-    return {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+torch = None   # (imported by the first call: the package loads without it)
+_TYPES = _HALVES = _INTS = _FLOAT = _INT = None
 
 
-def _require(ok, what):
-    if not ok:
-        raise ValueError(what)
+def _import():
+    global torch, _TYPES, _HALVES, _INTS, _FLOAT, _INT
+    import torch as module
+    _TYPES = {module.bfloat16: 0, module.float16: 1, module.float32: 2}
+    _HALVES = (module.bfloat16, module.float16)
+    _INTS, _FLOAT, _INT = (module.int32, module.int64), (module.float32,), (module.int32,)
+    torch = module
 
 
 def _tensor(t, name, device, shape=None, dtypes=None, rows=False):
     """Checks a CUDA tensor; rows: the last dimension adjacent, else contiguous."""
-    import torch
-    _require(isinstance(t, torch.Tensor) and t.is_cuda and t.device == device, f"{name}: a tensor on {device} is needed")
-    _require(dtypes is None or t.dtype in dtypes, f"{name}: type {t.dtype}, expected one of {dtypes}")
-    _require(shape is None or tuple(t.shape) == tuple(shape), f"{name}: shape {tuple(t.shape)}, expected {None if shape is None else tuple(shape)}")
-    if rows:
-        _require(t.shape[-1] <= 1 or t.stride(-1) == 1, f"{name}: the elements of its last dimension have to be adjacent")
-    else:
-        _require(t.is_contiguous(), f"{name}: has to be contiguous")
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise ValueError(f"{name}: a tensor on {device} is needed")
+    if dtypes is not None and t.dtype not in dtypes:
+        raise ValueError(f"{name}: type {t.dtype}, expected one of {tuple(dtypes)}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous() and not (rows and (t.shape[-1] <= 1 or t.stride(-1) == 1)):
+        raise ValueError(f"{name}: the elements of its last dimension have to be adjacent" if rows else f"{name}: has to be contiguous")
     return t
 
 
 def _device(t, name):
-    import torch
-    _require(isinstance(t, torch.Tensor) and t.is_cuda, f"{name}: a CUDA tensor is needed")
+    if torch is None:
+        _import()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name}: a CUDA tensor is needed")
     return t.device
 
 
@@ -92,8 +98,7 @@ def _matrix_stride(t):
 
 
 def _tokens(t, name, device, shape=None):
-    import torch
-    _tensor(t, name, device, shape, (torch.int32, torch.int64))
+    _tensor(t, name, device, shape, _INTS)
     return int(t.dtype == torch.int64)
 
 
@@ -101,12 +106,12 @@ class _Stream:
     """The stream of a call; one that is handed in is current while the call's tensors are allocated, so that their memory belongs to it."""
 
     def __init__(self, stream, device):
-        import torch
         self.device, self.context = device, None
         if stream is None:
-            self.stream = torch.cuda.current_stream(device)
+            self.stream = torch.cuda.current_stream(device.index)
         else:
-            _require(stream.device == device, f"the stream is one of {stream.device}, the tensors are on {device}")
+            if stream.device != device:
+                raise ValueError(f"the stream is one of {stream.device}, the tensors are on {device}")
             self.stream, self.context = stream, torch.cuda.stream(stream)
 
     def __enter__(self):
@@ -118,23 +123,23 @@ class _Stream:
         return self.context.__exit__(*exc) if self.context is not None else None
 
     def empty(self, *shape, dtype):
-        import torch
         return torch.empty(shape, dtype=dtype, device=self.device)
 
-    def workspace(self, given, nbytes):
-        import torch
-        if given is None:
-            return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.device)
-        return _tensor(given, "workspace", self.device)
+    def room(self, workspace, nbytes):
+        """Place and size of the call's workspace (16 bytes or fewer: none is looked at)."""
+        if workspace is not None:
+            _tensor(workspace, "workspace", self.device)
+        elif nbytes <= 16:
+            return None, 0
+        else:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self.kept = workspace
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
     def call(self, name, *args):
         rc = getattr(_lib(), "fpsched_op_" + name)(self.device.index, *args, self.stream.cuda_stream)
         if rc != 0:
             raise FpschedError(rc, "fpsched_op_" + name)
-
-
-def _room(workspace):
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _ptr(t):
@@ -147,8 +152,9 @@ def embedding(table, tokens, scale: float = 1.0, out=None, stream=None):
     """scale * table[tokens], with zeros for tokens outside the table (-1 for padding).  table: [rows][width], rows any distance
     apart; tokens: int32 or int64, any shape.  Returns [*tokens.shape][width] of the table's type."""
     device = _device(table, "table")
-    _require(table.dim() == 2, "table: two dimensions are needed")
-    _tensor(table, "table", device, dtypes=tuple(_types()), rows=True)
+    if table.dim() != 2:
+        raise ValueError("table: two dimensions are needed")
+    _tensor(table, "table", device, dtypes=_TYPES, rows=True)
     wide = _tokens(tokens, "tokens", device)
     with _Stream(stream, device) as s:
         shape = (*tokens.shape, table.shape[1])
@@ -156,7 +162,7 @@ def embedding(table, tokens, scale: float = 1.0, out=None, stream=None):
             out = s.empty(*shape, dtype=table.dtype)
         else:
             _tensor(out, "out", device, shape, (table.dtype,))
-        s.call("embedding", _types()[table.dtype], table.data_ptr(), _matrix_stride(table), table.shape[0], table.shape[1],
+        s.call("embedding", _TYPES[table.dtype], table.data_ptr(), _matrix_stride(table), table.shape[0], table.shape[1],
                tokens.data_ptr(), wide, tokens.numel(), float(scale), out.data_ptr(), table.shape[1])
     return out
 
@@ -165,24 +171,26 @@ def embedding_grad(grad, tokens, rows: int, scale: float = 1.0, out=None, accumu
     """The gradient of an embedding table of ``rows`` rows: every row's sum of the gradients of its tokens, times scale.  grad:
     [n][width] with rows any distance apart, or [*tokens.shape][width] contiguous; out: [rows][width] of grad's type (the default) or
     float32; accumulate: added to a float32 ``out`` (micro-batch by micro-batch) instead of written.  The same bits every time."""
-    import torch
     device = _device(grad, "grad")
     wide = _tokens(tokens, "tokens", device)
     rows = int(rows)
-    _require(rows >= 0, "rows: not negative")
-    _require(grad.dim() >= 2 and tuple(grad.shape[:-1]) == tuple(tokens.shape), "grad: one row for every token")
-    _tensor(grad, "grad", device, dtypes=tuple(_types()), rows=grad.dim() == 2)
+    if not (rows >= 0):
+        raise ValueError("rows: not negative")
+    if not (grad.dim() >= 2 and tuple(grad.shape[:-1]) == tuple(tokens.shape)):
+        raise ValueError("grad: one row for every token")
+    _tensor(grad, "grad", device, dtypes=_TYPES, rows=grad.dim() == 2)
     width = grad.shape[-1]
     flat = grad if grad.dim() == 2 else grad.reshape(-1, width)
-    _require(not accumulate or out is not None and out.dtype == torch.float32, "accumulate: needs a float32 out")
+    if not (not accumulate or out is not None and out.dtype == torch.float32):
+        raise ValueError("accumulate: needs a float32 out")
     with _Stream(stream, device) as s:
         if out is None:
             out = s.empty(rows, width, dtype=grad.dtype)
         else:
             _tensor(out, "out", device, (rows, width), (grad.dtype, torch.float32), rows=True)
-        room = s.workspace(workspace, _lib().fpsched_op_embedding_grad_workspace_bytes(rows, width, tokens.numel()))
-        s.call("embedding_grad", _types()[grad.dtype], flat.data_ptr(), _matrix_stride(flat), rows, width, tokens.data_ptr(), wide,
-               tokens.numel(), float(scale), _types()[out.dtype], out.data_ptr(), _matrix_stride(out), int(accumulate), *_room(room))
+        room = s.room(workspace, _lib().fpsched_op_embedding_grad_workspace_bytes(rows, width, tokens.numel()))
+        s.call("embedding_grad", _TYPES[grad.dtype], flat.data_ptr(), _matrix_stride(flat), rows, width, tokens.data_ptr(), wide,
+               tokens.numel(), float(scale), _TYPES[out.dtype], out.data_ptr(), _matrix_stride(out), int(accumulate), *room)
     return out
 
 
@@ -202,18 +210,17 @@ def gated_recurrence(gate, value, state=None, lengths=None, keep: bool = False, 
     sequence (behind them the output is zero and the state stands still).  Returns dict(out, state: float32 [batch][width] behind
     the last step, kept: with ``keep``, what ``gated_recurrence_grad`` needs).  ``final_state`` may be ``state`` itself: a serving
     loop calls this with one step at a time."""
-    import torch
     device = _device(value, "value")
-    _require(value.dim() == 3, "value: [batch][steps][width]")
+    if not (value.dim() == 3):
+        raise ValueError("value: [batch][steps][width]")
     n, steps, width = value.shape
-    kinds = tuple(_types())
-    _tensor(value, "value", device, dtypes=kinds, rows=True)
+    _tensor(value, "value", device, dtypes=_TYPES, rows=True)
     _tensor(gate, "gate", device, (n, steps, width), (value.dtype,), rows=True)
     for name, t in (("state", state), ("final_state", final_state)):
         if t is not None:
-            _tensor(t, name, device, (n, width), (torch.float32,))
+            _tensor(t, name, device, (n, width), _FLOAT)
     if lengths is not None:
-        _tensor(lengths, "lengths", device, (n,), (torch.int32,))
+        _tensor(lengths, "lengths", device, (n,), _INT)
     with _Stream(stream, device) as s:
         if out is None:
             out = s.empty(n, steps, width, dtype=value.dtype)
@@ -222,46 +229,46 @@ def gated_recurrence(gate, value, state=None, lengths=None, keep: bool = False, 
         if final_state is None:
             final_state = s.empty(n, width, dtype=torch.float32)
         kept = s.empty(n, -(-steps // BLOCK), width, dtype=torch.float32) if keep else None
-        room = s.workspace(workspace, _lib().fpsched_op_recurrence_workspace_bytes(n, steps, width))
-        s.call("recurrence", _types()[value.dtype], n, steps, width, gate.data_ptr(), value.data_ptr(), _steps(gate, value, out), _ptr(state),
-               _ptr(lengths), out.data_ptr(), final_state.data_ptr(), _ptr(kept), *_room(room))
+        room = s.room(workspace, _lib().fpsched_op_recurrence_workspace_bytes(n, steps, width))
+        s.call("recurrence", _TYPES[value.dtype], n, steps, width, gate.data_ptr(), value.data_ptr(), _steps(gate, value, out), _ptr(state),
+               _ptr(lengths), out.data_ptr(), final_state.data_ptr(), _ptr(kept), *room)
     return dict(out=out, state=final_state, **({"kept": kept} if keep else {}))
 
 
 def gated_recurrence_grad(grad, gate, value, kept, grad_state=None, lengths=None, workspace=None, stream=None):
     """Gradients of ``gated_recurrence`` (called with ``keep`` on the same gate, value, state and lengths): grad is that of its output,
     grad_state (float32 [batch][width], default: zero) that of its final state.  Returns dict(gate, value, state)."""
-    import torch
     device = _device(value, "value")
-    _require(value.dim() == 3, "value: [batch][steps][width]")
+    if not (value.dim() == 3):
+        raise ValueError("value: [batch][steps][width]")
     n, steps, width = value.shape
-    _tensor(value, "value", device, dtypes=tuple(_types()), rows=True)
+    _tensor(value, "value", device, dtypes=_TYPES, rows=True)
     for name, t in (("gate", gate), ("grad", grad)):
         _tensor(t, name, device, (n, steps, width), (value.dtype,), rows=True)
-    _tensor(kept, "kept", device, (n, -(-steps // BLOCK), width), (torch.float32,))
+    _tensor(kept, "kept", device, (n, -(-steps // BLOCK), width), _FLOAT)
     if grad_state is not None:
-        _tensor(grad_state, "grad_state", device, (n, width), (torch.float32,))
+        _tensor(grad_state, "grad_state", device, (n, width), _FLOAT)
     if lengths is not None:
-        _tensor(lengths, "lengths", device, (n,), (torch.int32,))
+        _tensor(lengths, "lengths", device, (n,), _INT)
     with _Stream(stream, device) as s:
         d_gate, d_value = (s.empty(n, steps, width, dtype=value.dtype) for _ in range(2))
         d_state = s.empty(n, width, dtype=torch.float32)
-        room = s.workspace(workspace, _lib().fpsched_op_recurrence_workspace_bytes(n, steps, width))
-        s.call("recurrence_grad", _types()[value.dtype], n, steps, width, grad.data_ptr(), gate.data_ptr(), value.data_ptr(),
+        room = s.room(workspace, _lib().fpsched_op_recurrence_workspace_bytes(n, steps, width))
+        s.call("recurrence_grad", _TYPES[value.dtype], n, steps, width, grad.data_ptr(), gate.data_ptr(), value.data_ptr(),
                _steps(grad, gate, value, d_gate, d_value), kept.data_ptr(), _ptr(grad_state), _ptr(lengths), d_gate.data_ptr(),
-               d_value.data_ptr(), d_state.data_ptr(), *_room(room))
+               d_value.data_ptr(), d_state.data_ptr(), *room)
     return dict(gate=d_gate, value=d_value, state=d_state)
 
 
 # ---- gated feed-forward block ----------------------------------------------------------------------------------------
 
 def _ffn_sizes(x, name, w_in, w_out, device):
-    import torch
-    kinds = (torch.bfloat16, torch.float16)
-    _require(x.dim() == 2, f"{name}: [tokens][width]")
+    if not (x.dim() == 2):
+        raise ValueError(f"{name}: [tokens][width]")
     tokens, width = x.shape
-    _tensor(x, name, device, dtypes=kinds, rows=True)
-    _require(w_in.dim() == 2 and w_in.shape[0] % 2 == 0, "w_in: [2 hidden][width]")
+    _tensor(x, name, device, dtypes=_HALVES, rows=True)
+    if not (w_in.dim() == 2 and w_in.shape[0] % 2 == 0):
+        raise ValueError("w_in: [2 hidden][width]")
     hidden = w_in.shape[0] // 2
     _tensor(w_in, "w_in", device, (2 * hidden, width), (x.dtype,))
     _tensor(w_out, "w_out", device, (width, hidden), (x.dtype,))
@@ -270,16 +277,19 @@ def _ffn_sizes(x, name, w_in, w_out, device):
 
 
 def _multiples_of_8(width, hidden):
-    _require(width > 0 and hidden > 0 and width % 8 == 0 and hidden % 8 == 0, "width and hidden width: multiples of 8")
+    if not (width > 0 and hidden > 0 and width % 8 == 0 and hidden % 8 == 0):
+        raise ValueError("width and hidden width: multiples of 8")
 
 
 def _rows_of_16_bytes(**tensors):
     for name, t in tensors.items():
-        _require(t.data_ptr() % 16 == 0 and _matrix_stride(t) % 8 == 0, f"{name}: its rows have to begin at multiples of 16 bytes")
+        if not (t.data_ptr() % 16 == 0 and _matrix_stride(t) % 8 == 0):
+            raise ValueError(f"{name}: its rows have to begin at multiples of 16 bytes")
 
 
 def _activation(name):
-    _require(name in _ACTIVATIONS, f"activation: one of {sorted(_ACTIVATIONS)}")
+    if not (name in _ACTIVATIONS):
+        raise ValueError(f"activation: one of {sorted(_ACTIVATIONS)}")
     return _ACTIVATIONS[name]
 
 
@@ -298,9 +308,9 @@ def gated_ffn(x, w_in, w_out, activation: str = "silu", keep: bool = False, out=
         _rows_of_16_bytes(x=x, w_in=w_in, w_out=w_out, out=out)
         pre = s.empty(tokens, 2 * hidden, dtype=x.dtype) if keep else None
         h = s.empty(tokens, hidden, dtype=x.dtype)
-        room = s.workspace(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
-        s.call("ffn", _types()[x.dtype], act, tokens, width, hidden, x.data_ptr(), _matrix_stride(x), w_in.data_ptr(), w_out.data_ptr(), _ptr(pre),
-               h.data_ptr(), out.data_ptr(), _matrix_stride(out), *_room(room))
+        room = s.room(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
+        s.call("ffn", _TYPES[x.dtype], act, tokens, width, hidden, x.data_ptr(), _matrix_stride(x), w_in.data_ptr(), w_out.data_ptr(), _ptr(pre),
+               h.data_ptr(), out.data_ptr(), _matrix_stride(out), *room)
     return dict(out=out, **({"kept": dict(pre=pre, hidden=h)} if keep else {}))
 
 
@@ -315,29 +325,30 @@ def gated_ffn_input_grad(grad, w_in, w_out, kept, activation: str = "silu", work
     with _Stream(stream, device) as s:
         d_x = s.empty(tokens, width, dtype=grad.dtype)
         d_pre = s.empty(tokens, 2 * hidden, dtype=grad.dtype)
-        room = s.workspace(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
-        s.call("ffn_input_grad", _types()[grad.dtype], act, tokens, width, hidden, grad.data_ptr(), _matrix_stride(grad), w_in.data_ptr(),
-               w_out.data_ptr(), pre.data_ptr(), d_pre.data_ptr(), d_x.data_ptr(), width, *_room(room))
+        room = s.room(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
+        s.call("ffn_input_grad", _TYPES[grad.dtype], act, tokens, width, hidden, grad.data_ptr(), _matrix_stride(grad), w_in.data_ptr(),
+               w_out.data_ptr(), pre.data_ptr(), d_pre.data_ptr(), d_x.data_ptr(), width, *room)
     return dict(x=d_x, kept=dict(pre=d_pre))
 
 
 def gated_ffn_weight_grad(x, grad, kept, grad_kept, out=None, accumulate: bool = False, workspace=None, stream=None):
     """The W item: the weights' gradients from x, the output's gradient, what ``gated_ffn`` kept and what ``gated_ffn_input_grad``
     kept.  out: dict(w_in, w_out) of tensors of x's type or, both, float32; accumulate: added to float32 ones.  Returns them."""
-    import torch
     device = _device(x, "x")
-    kinds = (torch.bfloat16, torch.float16)
-    _require(x.dim() == 2, "x: [tokens][width]")
+    if not (x.dim() == 2):
+        raise ValueError("x: [tokens][width]")
     tokens, width = x.shape
-    _tensor(x, "x", device, dtypes=kinds, rows=True)
+    _tensor(x, "x", device, dtypes=_HALVES, rows=True)
     _tensor(grad, "grad", device, (tokens, width), (x.dtype,), rows=True)
     h = kept["hidden"]
-    _require(h.dim() == 2, "kept: of another call")
+    if not (h.dim() == 2):
+        raise ValueError("kept: of another call")
     hidden = h.shape[1]
     _multiples_of_8(width, hidden)
     _tensor(h, "kept", device, (tokens, hidden), (x.dtype,))
     d_pre = _tensor(grad_kept["pre"], "grad_kept", device, (tokens, 2 * hidden), (x.dtype,))
-    _require(not accumulate or out is not None and out["w_in"].dtype == torch.float32, "accumulate: needs float32 outputs")
+    if not (not accumulate or out is not None and out["w_in"].dtype == torch.float32):
+        raise ValueError("accumulate: needs float32 outputs")
     with _Stream(stream, device) as s:
         if out is None:
             out = dict(w_in=s.empty(2 * hidden, width, dtype=x.dtype), w_out=s.empty(width, hidden, dtype=x.dtype))
@@ -345,9 +356,9 @@ def gated_ffn_weight_grad(x, grad, kept, grad_kept, out=None, accumulate: bool =
         _tensor(out["w_in"], "out", device, (2 * hidden, width), (x.dtype, torch.float32))
         _tensor(out["w_out"], "out", device, (width, hidden), (kind,))
         _rows_of_16_bytes(x=x, grad=grad, kept=h, grad_kept=d_pre, w_in=out["w_in"], w_out=out["w_out"])
-        room = s.workspace(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
-        s.call("ffn_weight_grad", _types()[x.dtype], tokens, width, hidden, x.data_ptr(), _matrix_stride(x), grad.data_ptr(), _matrix_stride(grad),
-               h.data_ptr(), d_pre.data_ptr(), _types()[kind], out["w_in"].data_ptr(), out["w_out"].data_ptr(), int(accumulate), *_room(room))
+        room = s.room(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
+        s.call("ffn_weight_grad", _TYPES[x.dtype], tokens, width, hidden, x.data_ptr(), _matrix_stride(x), grad.data_ptr(), _matrix_stride(grad),
+               h.data_ptr(), d_pre.data_ptr(), _TYPES[kind], out["w_in"].data_ptr(), out["w_out"].data_ptr(), int(accumulate), *room)
     return out
 
 
@@ -359,44 +370,45 @@ def token_logprobs(logits, tokens, alternatives: int = 0, workspace=None, stream
     two parts (largest logit, rest), and with ``alternatives`` = k > 0 the k largest logits of each row, of equal ones the
     lowest id first, as ids: int32 [rows][k] and logprobs: float32 [rows][k]; -1 and -inf where fewer are not masked).  A logit of
     -inf is masked; a row with nothing else has logprob -inf and entropy 0; one with NaN or +inf is NaN throughout."""
-    import torch
     device = _device(logits, "logits")
-    _require(logits.dim() == 2 and logits.shape[1] > 0, "logits: [rows][vocab]")
+    if not (logits.dim() == 2 and logits.shape[1] > 0):
+        raise ValueError("logits: [rows][vocab]")
     n, vocab = logits.shape
-    _tensor(logits, "logits", device, dtypes=tuple(_types()), rows=True)
+    _tensor(logits, "logits", device, dtypes=_TYPES, rows=True)
     wide = _tokens(tokens, "tokens", device, (n,))
     k = int(alternatives)
-    _require(0 <= k <= MAX_ALTERNATIVES, f"alternatives: 0 to {MAX_ALTERNATIVES}")
+    if not (0 <= k <= MAX_ALTERNATIVES):
+        raise ValueError(f"alternatives: 0 to {MAX_ALTERNATIVES}")
     with _Stream(stream, device) as s:
         done = dict(logprob=s.empty(n, dtype=torch.float32), entropy=s.empty(n, dtype=torch.float32), lse=s.empty(n, 2, dtype=torch.float32))
         if k:
             done.update(ids=s.empty(n, k, dtype=torch.int32), logprobs=s.empty(n, k, dtype=torch.float32))
-        room = s.workspace(workspace, _lib().fpsched_op_logprobs_workspace_bytes(n, vocab, k))
-        s.call("logprobs", _types()[logits.dtype], n, vocab, logits.data_ptr(), _matrix_stride(logits), tokens.data_ptr(), wide, k,
+        room = s.room(workspace, _lib().fpsched_op_logprobs_workspace_bytes(n, vocab, k))
+        s.call("logprobs", _TYPES[logits.dtype], n, vocab, logits.data_ptr(), _matrix_stride(logits), tokens.data_ptr(), wide, k,
                done["logprob"].data_ptr(), done["entropy"].data_ptr(), done["lse"].data_ptr(), _ptr(done.get("ids")), _ptr(done.get("logprobs")),
-               *_room(room))
+               *room)
     return done
 
 
 def token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, grad_entropy=None, out=None, stream=None):
     """The gradient of the logits from those of ``logprob`` and ``entropy`` (float32 [rows], None: zero) and what ``token_logprobs``
     returned.  out: of the logits' type, may be ``logits`` itself.  Returns it."""
-    import torch
     device = _device(logits, "logits")
-    _require(logits.dim() == 2 and logits.shape[1] > 0, "logits: [rows][vocab]")
+    if not (logits.dim() == 2 and logits.shape[1] > 0):
+        raise ValueError("logits: [rows][vocab]")
     n, vocab = logits.shape
-    _tensor(logits, "logits", device, dtypes=tuple(_types()), rows=True)
+    _tensor(logits, "logits", device, dtypes=_TYPES, rows=True)
     wide = _tokens(tokens, "tokens", device, (n,))
-    _tensor(lse, "lse", device, (n, 2), (torch.float32,))
-    _tensor(entropy, "entropy", device, (n,), (torch.float32,))
+    _tensor(lse, "lse", device, (n, 2), _FLOAT)
+    _tensor(entropy, "entropy", device, (n,), _FLOAT)
     for name, t in (("grad_logprob", grad_logprob), ("grad_entropy", grad_entropy)):
         if t is not None:
-            _tensor(t, name, device, (n,), (torch.float32,))
+            _tensor(t, name, device, (n,), _FLOAT)
     with _Stream(stream, device) as s:
         if out is None:
             out = s.empty(n, vocab, dtype=logits.dtype)
         else:
             _tensor(out, "out", device, (n, vocab), (logits.dtype,), rows=True)
-        s.call("logprobs_grad", _types()[logits.dtype], n, vocab, logits.data_ptr(), _matrix_stride(logits), tokens.data_ptr(), wide, lse.data_ptr(),
+        s.call("logprobs_grad", _TYPES[logits.dtype], n, vocab, logits.data_ptr(), _matrix_stride(logits), tokens.data_ptr(), wide, lse.data_ptr(),
                entropy.data_ptr(), _ptr(grad_logprob), _ptr(grad_entropy), out.data_ptr(), _matrix_stride(out))
     return out
