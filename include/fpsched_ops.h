@@ -85,31 +85,33 @@ int fpsched_op_recurrence_grad(int device_id, int type, int64_t n_batch, int64_t
 /* ---- gated feed-forward block -------------------------------------------------------------------
  * [g u] = x w_in^T,  hidden = act(g) u,  out = hidden w_out^T.  x, out: [n_tokens][width], rows x_stride
  * and out_stride apart; w_in: [2 hidden_width][width], the gate's rows first; w_out: [width][hidden_width];
- * pre (NULL, or [n_tokens][2 hidden_width]): g and u, for the backward pass; hidden: [n_tokens][hidden_width].
- * Types FPSCHED_BF16 and FPSCHED_F16, the same for all; weights, pre and hidden contiguous.  width,
- * hidden_width and the strides are multiples of 8, the tensors 16-byte aligned (FPSCHED_EINVAL): rows are
- * moved 16 bytes at a time.  act is computed in 32 bits from unrounded g and u. */
+ * hidden: [n_tokens][hidden_width], free again when the call's work is done; kept: NULL, or
+ * FPSCHED_FFN_KEPT_BYTES of g and u in 24 bits for the backward pass.  Types FPSCHED_BF16 and FPSCHED_F16, the
+ * same for all; weights and hidden contiguous.  width, hidden_width and the strides are multiples of 8,
+ * the tensors 16-byte aligned (FPSCHED_EINVAL): rows are moved 16 bytes at a time.  act is computed in 32
+ * bits from unrounded g and u. */
 enum { FPSCHED_SILU = 0, FPSCHED_GELU = 1 /* with tanh */, FPSCHED_RELU = 2 };
+#define FPSCHED_FFN_KEPT_BYTES(n_tokens, hidden_width) ((size_t)6 * (n_tokens) * (hidden_width))
 size_t fpsched_op_ffn_workspace_bytes(int64_t n_tokens, int64_t width, int64_t hidden_width);
 int fpsched_op_ffn(int device_id, int type, int act, int64_t n_tokens, int64_t width, int64_t hidden_width,
-                   const void *x, int64_t x_stride, const void *w_in, const void *w_out, void *pre,
+                   const void *x, int64_t x_stride, const void *w_in, const void *w_out, void *kept,
                    void *hidden, void *out, int64_t out_stride, void *d_workspace, size_t workspace_bytes,
                    void *hip_stream);
 
-/* The B item: d_hidden = grad w_out, d_pre = [d_hidden u act'(g), d_hidden act(g)] (of `type`, from the kept
- * pre), d_x = d_pre w_in. */
+/* The B item: d_hidden = grad w_out, d_pre = [d_hidden u act'(g), d_hidden act(g)] (rounded to `type`),
+ * d_x = d_pre w_in.  kept: what the F item wrote; on return it holds d_pre, [n_tokens][2 hidden_width] of
+ * `type`, and behind it hidden again, [n_tokens][hidden_width], for the W item.  So it serves one B item. */
 int fpsched_op_ffn_input_grad(int device_id, int type, int act, int64_t n_tokens, int64_t width,
                               int64_t hidden_width, const void *grad, int64_t grad_stride, const void *w_in,
-                              const void *w_out, const void *pre, void *d_pre, void *d_x, int64_t d_x_stride,
+                              const void *w_out, void *kept, void *d_x, int64_t d_x_stride,
                               void *d_workspace, size_t workspace_bytes, void *hip_stream);
 
 /* The W item: d_w_in = d_pre^T x, d_w_out = grad^T hidden, of `type` or FPSCHED_F32; with accumulate
- * (FPSCHED_F32 only) added to what is there. */
+ * (FPSCHED_F32 only) added to what is there.  kept: as the B item left it. */
 int fpsched_op_ffn_weight_grad(int device_id, int type, int64_t n_tokens, int64_t width, int64_t hidden_width,
                                const void *x, int64_t x_stride, const void *grad, int64_t grad_stride,
-                               const void *hidden, const void *d_pre, int out_type, void *d_w_in,
-                               void *d_w_out, int accumulate, void *d_workspace, size_t workspace_bytes,
-                               void *hip_stream);
+                               const void *kept, int out_type, void *d_w_in, void *d_w_out, int accumulate,
+                               void *d_workspace, size_t workspace_bytes, void *hip_stream);
 
 /* ---- log probabilities of given tokens ------------------------------------------------------------
  * Per row of logits ([n_rows][vocab], rows logits_stride apart), with p = softmax:

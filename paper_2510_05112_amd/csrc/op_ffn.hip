@@ -54,7 +54,7 @@ struct Gemm {
   int64_t out_stride;
   int accumulate;
   int act;
-  void* pre;                 // kGated: written unless NULL; kGatedGrad: read
+  void* kept;                // kGated: written unless NULL; kGatedGrad: read, and written in its place
   int tiles_m, tiles_n;
   int64_t part_depth;        // kPart: a part's k
 };
@@ -183,40 +183,77 @@ __device__ __forceinline__ void tile_of(unsigned id, int tiles_m, int tiles_n, i
   *tn = in / high;
 }
 
-// What becomes of 8 neighbouring columns of a row, of the gate's half and the other one.
-template <typename T>
-__device__ __forceinline__ void put_gated(const Gemm& a, int64_t m, int64_t n, const Vec<float, 8>& gate, const Vec<float, 8>& up) {
-  Vec<T, 8> h, g, u;
+// What the forward pass keeps: g and u in 24 bits (a 32-bit number's first 24, rounded), off by 2^-16 of themselves at most.  In 16 bits they would
+// add as much to the gradients' error as rounding d_pre does (bfloat16, 8,192 x 4,096 x 10,752: 3.0e-3 of the gradients' norm, and 2.4e-3 so).  The
+// first 16 of all are [m][2 n_half], as d_pre will be; the last 8 of g and u are side by side in [m][n_half][2], where the same element of
+// hidden will be: the backward pass writes the three in the place of the two, whose memory then lasts until the weights' gradients.
+template <int N>
+struct Kept {
+  Vec<unsigned short, N> g, u;
+  Vec<unsigned char, 2 * N> last;
+
+  static __device__ __forceinline__ unsigned bits(float x) { return x == x ? __float_as_uint(x) + 0x80u : 0x7fc00000u; }
+  __device__ __forceinline__ void set(int e, float gate, float up) {
+    const unsigned bg = bits(gate), bu = bits(up);
+    g.at[e] = (unsigned short)(bg >> 16);
+    u.at[e] = (unsigned short)(bu >> 16);
+    last.at[2 * e] = (unsigned char)(bg >> 8);
+    last.at[2 * e + 1] = (unsigned char)(bu >> 8);
+  }
+  __device__ __forceinline__ float gate(int e) const { return __uint_as_float((unsigned)g.at[e] << 16 | (unsigned)last.at[2 * e] << 8); }
+  __device__ __forceinline__ float up(int e) const { return __uint_as_float((unsigned)u.at[e] << 16 | (unsigned)last.at[2 * e + 1] << 8); }
+
+  static __device__ __forceinline__ unsigned short* first_of(const Gemm& a, int64_t m, int64_t n) {
+    return static_cast<unsigned short*>(a.kept) + m * 2 * a.n_half + n;
+  }
+  static __device__ __forceinline__ unsigned char* last_of(const Gemm& a, int64_t m, int64_t n) {
+    return static_cast<unsigned char*>(a.kept) + (a.m.extent * 2 + m) * 2 * a.n_half + 2 * n;
+  }
+  __device__ __forceinline__ void store(const Gemm& a, int64_t m, int64_t n) const {
+    store_vec<unsigned short, N>(first_of(a, m, n), g);
+    store_vec<unsigned short, N>(first_of(a, m, n) + a.n_half, u);
+    store_vec<unsigned char, 2 * N>(last_of(a, m, n), last);
+  }
+  __device__ __forceinline__ void load(const Gemm& a, int64_t m, int64_t n) {
+    g = load_vec<unsigned short, N>(first_of(a, m, n));
+    u = load_vec<unsigned short, N>(first_of(a, m, n) + a.n_half);
+    last = load_vec<unsigned char, 2 * N>(last_of(a, m, n));
+  }
+};
+
+// What becomes of N neighbouring columns of a row, of the gate's half and the other one.
+template <typename T, int N>
+__device__ __forceinline__ void put_gated(const Gemm& a, int64_t m, int64_t n, const Vec<float, N>& gate, const Vec<float, N>& up) {
+  Vec<T, N> h;
+  Kept<N> kept;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < N; ++e) {
     h.at[e] = (T)(activate(a.act, gate.at[e]) * up.at[e]);
-    g.at[e] = (T)gate.at[e];
-    u.at[e] = (T)up.at[e];
+    kept.set(e, gate.at[e], up.at[e]);
   }
-  store_vec<T, 8>(static_cast<T*>(a.out) + m * a.out_stride + n, h);
-  if (a.pre) {
-    T* pre = static_cast<T*>(a.pre) + m * 2 * a.n_half + n;
-    store_vec<T, 8>(pre, g);
-    store_vec<T, 8>(pre + a.n_half, u);
-  }
+  store_vec<T, N>(static_cast<T*>(a.out) + m * a.out_stride + n, h);
+  if (a.kept) kept.store(a, m, n);
 }
 
 // ... of 8 neighbouring columns of a row where there are no halves.
 template <typename T, int EPILOGUE, typename O>
 __device__ __forceinline__ void put_columns(const Gemm& a, int64_t m, int64_t n, const Vec<float, 8>& x) {
   if constexpr (EPILOGUE == kGatedGrad) {
-    const T* pre = static_cast<const T*>(a.pre) + m * 2 * a.n_half + n;
-    const Vec<T, 8> g = load_vec<T, 8>(pre), u = load_vec<T, 8>(pre + a.n_half);
-    Vec<T, 8> dg, du;
+    Kept<8> kept;
+    kept.load(a, m, n);
+    asm volatile("" : : : "memory");   // (what is written below is of another type, in the same place)
+    Vec<T, 8> dg, du, h;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float gate = (float)g.at[e];
-      dg.at[e] = (T)(x.at[e] * (float)u.at[e] * slope(a.act, gate));
-      du.at[e] = (T)(x.at[e] * activate(a.act, gate));
+      const float gate = kept.gate(e), up = kept.up(e), act = activate(a.act, gate);
+      dg.at[e] = (T)(x.at[e] * up * slope(a.act, gate));
+      du.at[e] = (T)(x.at[e] * act);
+      h.at[e] = (T)(act * up);
     }
-    T* out = static_cast<T*>(a.out) + m * a.out_stride + n;
+    T* out = reinterpret_cast<T*>(Kept<8>::first_of(a, m, n));
     store_vec<T, 8>(out, dg);
     store_vec<T, 8>(out + a.n_half, du);
+    store_vec<T, 8>(reinterpret_cast<T*>(Kept<8>::last_of(a, m, n)), h);
   } else {
     O* out = static_cast<O*>(a.out) + m * a.out_stride + n;
     Vec<O, 8> v = {};
@@ -344,7 +381,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
       if constexpr (kHalves) {
         const Vec<float, 4> u0 = load_vec<float, 4>(from + kColumns), u1 = load_vec<float, 4>(from + kColumns + 4);
         if (m >= a.m.extent || n >= a.n_half) continue;
-        put_gated<T>(a, m, n, {x0.at[0], x0.at[1], x0.at[2], x0.at[3], x1.at[0], x1.at[1], x1.at[2], x1.at[3]},
+        put_gated<T, 8>(a, m, n, {x0.at[0], x0.at[1], x0.at[2], x0.at[3], x1.at[0], x1.at[1], x1.at[2], x1.at[3]},
                      {u0.at[0], u0.at[1], u0.at[2], u0.at[3], u1.at[0], u1.at[1], u1.at[2], u1.at[3]});
       } else {
         if (m >= a.m.extent || n >= a.n.extent) continue;
@@ -428,19 +465,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(Gemm a) {
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) total[s] += *reinterpret_cast<const f32x4*>(sums[w][s][lane]);
   if constexpr (EPILOGUE == kGated) {
-    Vec<T, 4> h, g, u;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      h.at[e] = (T)(activate(a.act, total[0][e]) * total[1][e]);
-      g.at[e] = (T)total[0][e];
-      u.at[e] = (T)total[1][e];
-    }
-    store_vec<T, 4>(static_cast<T*>(a.out) + m * a.out_stride + n, h);
-    if (a.pre) {
-      T* pre = static_cast<T*>(a.pre) + m * 2 * a.n_half + n;
-      store_vec<T, 4>(pre, g);
-      store_vec<T, 4>(pre + a.n_half, u);
-    }
+    put_gated<T, 4>(a, m, n, {total[0][0], total[0][1], total[0][2], total[0][3]}, {total[1][0], total[1][1], total[1][2], total[1][3]});
   } else {
     store_vec<T, 4>(static_cast<T*>(a.out) + m * a.out_stride + n, {(T)total[0][0], (T)total[0][1], (T)total[0][2], (T)total[0][3]});
   }
@@ -476,7 +501,7 @@ __global__ __launch_bounds__(256) void add_parts_kernel(Gemm a, const float* par
     }
     return sum;
   };
-  if constexpr (EPILOGUE == kGated) put_gated<T>(a, m, n, total(n), total(a.n_half + n));
+  if constexpr (EPILOGUE == kGated) put_gated<T, 8>(a, m, n, total(n), total(a.n_half + n));
   else put_columns<T, EPILOGUE, O>(a, m, n, total(n));
 }
 
@@ -580,12 +605,12 @@ size_t fpsched_op_ffn_workspace_bytes(int64_t n_tokens, int64_t width, int64_t h
 }
 
 int fpsched_op_ffn(int device_id, int type, int act, int64_t n_tokens, int64_t width, int64_t hidden_width, const void* x,
-                   int64_t x_stride, const void* w_in, const void* w_out, void* pre, void* hidden, void* out, int64_t out_stride,
+                   int64_t x_stride, const void* w_in, const void* w_out, void* kept, void* hidden, void* out, int64_t out_stride,
                    void* d_workspace, size_t workspace_bytes, void* hip_stream) {
   if (check_sizes(type, act, n_tokens, width, hidden_width) != FPSCHED_OK || x_stride < width || out_stride < width) return FPSCHED_EINVAL;
   if (device_id < 0) return FPSCHED_ENODEV;
   if (n_tokens == 0) return FPSCHED_OK;
-  if (!row_ok(x, x_stride) || !row_ok(out, out_stride) || !row_ok(w_in, 0) || !row_ok(w_out, 0) || !row_ok(hidden, 0) || (pre && !aligned(pre, 16)))
+  if (!row_ok(x, x_stride) || !row_ok(out, out_stride) || !row_ok(w_in, 0) || !row_ok(w_out, 0) || !row_ok(hidden, 0) || (kept && !aligned(kept, 16)))
     return FPSCHED_EINVAL;
   const int room = check_workspace(d_workspace, workspace_bytes, n_tokens, width, hidden_width);
   if (room != FPSCHED_OK) return room;
@@ -596,7 +621,7 @@ int fpsched_op_ffn(int device_id, int type, int act, int64_t n_tokens, int64_t w
     using T = decltype(zero);
     Gemm a = {};
     a.m = {x, x_stride, n_tokens}; a.n = {w_in, width, 2 * hidden_width}; a.depth = width; a.n_half = hidden_width;
-    a.out = hidden; a.out_stride = hidden_width; a.act = act; a.pre = pre;
+    a.out = hidden; a.out_stride = hidden_width; a.act = act; a.kept = kept;
     const int first = n_tokens <= kFewRows ? few_rows<T, kGated>(a, stream) : gemm<T, kAlong, kAlong, kGated, T>(a, d_workspace, stream);
     if (first != FPSCHED_OK) return first;
     Gemm b = {};
@@ -607,12 +632,12 @@ int fpsched_op_ffn(int device_id, int type, int act, int64_t n_tokens, int64_t w
 }
 
 int fpsched_op_ffn_input_grad(int device_id, int type, int act, int64_t n_tokens, int64_t width, int64_t hidden_width,
-                              const void* grad, int64_t grad_stride, const void* w_in, const void* w_out, const void* pre,
-                              void* d_pre, void* d_x, int64_t d_x_stride, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+                              const void* grad, int64_t grad_stride, const void* w_in, const void* w_out, void* kept,
+                              void* d_x, int64_t d_x_stride, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
   if (check_sizes(type, act, n_tokens, width, hidden_width) != FPSCHED_OK || grad_stride < width || d_x_stride < width) return FPSCHED_EINVAL;
   if (device_id < 0) return FPSCHED_ENODEV;
   if (n_tokens == 0) return FPSCHED_OK;
-  if (!row_ok(grad, grad_stride) || !row_ok(d_x, d_x_stride) || !row_ok(w_in, 0) || !row_ok(w_out, 0) || !row_ok(pre, 0) || !row_ok(d_pre, 0))
+  if (!row_ok(grad, grad_stride) || !row_ok(d_x, d_x_stride) || !row_ok(w_in, 0) || !row_ok(w_out, 0) || !row_ok(kept, 0))
     return FPSCHED_EINVAL;
   const int room = check_workspace(d_workspace, workspace_bytes, n_tokens, width, hidden_width);
   if (room != FPSCHED_OK) return room;
@@ -623,25 +648,24 @@ int fpsched_op_ffn_input_grad(int device_id, int type, int act, int64_t n_tokens
     using T = decltype(zero);
     Gemm a = {};
     a.m = {grad, grad_stride, n_tokens}; a.n = {w_out, hidden_width, hidden_width}; a.depth = width; a.n_half = hidden_width;
-    a.out = d_pre; a.out_stride = 2 * hidden_width; a.act = act; a.pre = const_cast<void*>(pre);
+    a.act = act; a.kept = kept;
     const int first = gemm<T, kAlong, kDown, kGatedGrad, T>(a, d_workspace, stream);
     if (first != FPSCHED_OK) return first;
     Gemm b = {};
-    b.m = {d_pre, 2 * hidden_width, n_tokens}; b.n = {w_in, width, width}; b.depth = 2 * hidden_width;
+    b.m = {kept, 2 * hidden_width, n_tokens}; b.n = {w_in, width, width}; b.depth = 2 * hidden_width;
     b.out = d_x; b.out_stride = d_x_stride;
     return gemm<T, kAlong, kDown, kStore, T>(b, d_workspace, stream);
   });
 }
 
 int fpsched_op_ffn_weight_grad(int device_id, int type, int64_t n_tokens, int64_t width, int64_t hidden_width, const void* x,
-                               int64_t x_stride, const void* grad, int64_t grad_stride, const void* hidden, const void* d_pre,
-                               int out_type, void* d_w_in, void* d_w_out, int accumulate, void* d_workspace,
+                               int64_t x_stride, const void* grad, int64_t grad_stride, const void* kept, int out_type, void* d_w_in, void* d_w_out, int accumulate, void* d_workspace,
                                size_t workspace_bytes, void* hip_stream) {
   if (check_sizes(type, 0, n_tokens, width, hidden_width) != FPSCHED_OK || x_stride < width || grad_stride < width) return FPSCHED_EINVAL;
   if ((out_type != type && out_type != FPSCHED_F32) || (accumulate && out_type != FPSCHED_F32)) return FPSCHED_EINVAL;
   if (device_id < 0) return FPSCHED_ENODEV;
   if (!row_ok(d_w_in, 0) || !row_ok(d_w_out, 0)) return FPSCHED_EINVAL;
-  if (n_tokens > 0 && (!row_ok(x, x_stride) || !row_ok(grad, grad_stride) || !row_ok(hidden, 0) || !row_ok(d_pre, 0))) return FPSCHED_EINVAL;
+  if (n_tokens > 0 && (!row_ok(x, x_stride) || !row_ok(grad, grad_stride) || !row_ok(kept, 0))) return FPSCHED_EINVAL;
   if (n_tokens == 0 && accumulate) return FPSCHED_OK;
   const int room = check_workspace(d_workspace, workspace_bytes, n_tokens, width, hidden_width);
   if (room != FPSCHED_OK) return room;
@@ -658,12 +682,12 @@ int fpsched_op_ffn_weight_grad(int device_id, int type, int64_t n_tokens, int64_
         return launched();
       }
       Gemm a = {};
-      a.m = {d_pre, 2 * hidden_width, 2 * hidden_width}; a.n = {x, x_stride, width}; a.depth = n_tokens;
+      a.m = {kept, 2 * hidden_width, 2 * hidden_width}; a.n = {x, x_stride, width}; a.depth = n_tokens;
       a.out = d_w_in; a.out_stride = width; a.accumulate = accumulate;
       const int first = gemm<T, kDown, kDown, kStore, O>(a, d_workspace, stream);
       if (first != FPSCHED_OK) return first;
       Gemm b = {};
-      b.m = {grad, grad_stride, width}; b.n = {hidden, hidden_width, hidden_width}; b.depth = n_tokens;
+      b.m = {grad, grad_stride, width}; b.n = {static_cast<const T*>(kept) + n_tokens * 2 * hidden_width, hidden_width, hidden_width}; b.depth = n_tokens;
       b.out = d_w_out; b.out_stride = hidden_width; b.accumulate = accumulate;
       return gemm<T, kDown, kDown, kStore, O>(b, d_workspace, stream);
     };

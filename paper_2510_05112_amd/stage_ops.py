@@ -38,8 +38,8 @@ def _lib():
             "recurrence": [i32, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp] + ws,
             "recurrence_grad": [i32, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp] + ws,
             "ffn": [i32, i32, i32, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, i64] + ws,
-            "ffn_input_grad": [i32, i32, i32, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, i64] + ws,
-            "ffn_weight_grad": [i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, i32] + ws,
+            "ffn_input_grad": [i32, i32, i32, i64, i64, i64, vp, i64, vp, vp, vp, vp, i64] + ws,
+            "ffn_weight_grad": [i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, i32, vp, vp, i32] + ws,
             "logprobs": [i32, i32, i64, i64, vp, i64, vp, i32, i32, vp, vp, vp, vp, vp] + ws,
             "logprobs_grad": [i32, i32, i64, i64, vp, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp],
         }
@@ -174,14 +174,14 @@ def embedding_grad(grad, tokens, rows: int, scale: float = 1.0, out=None, accumu
     device = _device(grad, "grad")
     wide = _tokens(tokens, "tokens", device)
     rows = int(rows)
-    if not (rows >= 0):
+    if rows < 0:
         raise ValueError("rows: not negative")
-    if not (grad.dim() >= 2 and tuple(grad.shape[:-1]) == tuple(tokens.shape)):
+    if grad.dim() < 2 or grad.shape[:-1] != tokens.shape:
         raise ValueError("grad: one row for every token")
     _tensor(grad, "grad", device, dtypes=_TYPES, rows=grad.dim() == 2)
     width = grad.shape[-1]
     flat = grad if grad.dim() == 2 else grad.reshape(-1, width)
-    if not (not accumulate or out is not None and out.dtype == torch.float32):
+    if accumulate and (out is None or out.dtype != torch.float32):
         raise ValueError("accumulate: needs a float32 out")
     with _Stream(stream, device) as s:
         if out is None:
@@ -211,7 +211,7 @@ def gated_recurrence(gate, value, state=None, lengths=None, keep: bool = False, 
     the last step, kept: with ``keep``, what ``gated_recurrence_grad`` needs).  ``final_state`` may be ``state`` itself: a serving
     loop calls this with one step at a time."""
     device = _device(value, "value")
-    if not (value.dim() == 3):
+    if value.dim() != 3:
         raise ValueError("value: [batch][steps][width]")
     n, steps, width = value.shape
     _tensor(value, "value", device, dtypes=_TYPES, rows=True)
@@ -239,7 +239,7 @@ def gated_recurrence_grad(grad, gate, value, kept, grad_state=None, lengths=None
     """Gradients of ``gated_recurrence`` (called with ``keep`` on the same gate, value, state and lengths): grad is that of its output,
     grad_state (float32 [batch][width], default: zero) that of its final state.  Returns dict(gate, value, state)."""
     device = _device(value, "value")
-    if not (value.dim() == 3):
+    if value.dim() != 3:
         raise ValueError("value: [batch][steps][width]")
     n, steps, width = value.shape
     _tensor(value, "value", device, dtypes=_TYPES, rows=True)
@@ -263,11 +263,11 @@ def gated_recurrence_grad(grad, gate, value, kept, grad_state=None, lengths=None
 # ---- gated feed-forward block ----------------------------------------------------------------------------------------
 
 def _ffn_sizes(x, name, w_in, w_out, device):
-    if not (x.dim() == 2):
+    if x.dim() != 2:
         raise ValueError(f"{name}: [tokens][width]")
     tokens, width = x.shape
     _tensor(x, name, device, dtypes=_HALVES, rows=True)
-    if not (w_in.dim() == 2 and w_in.shape[0] % 2 == 0):
+    if w_in.dim() != 2 or w_in.shape[0] % 2:
         raise ValueError("w_in: [2 hidden][width]")
     hidden = w_in.shape[0] // 2
     _tensor(w_in, "w_in", device, (2 * hidden, width), (x.dtype,))
@@ -277,26 +277,42 @@ def _ffn_sizes(x, name, w_in, w_out, device):
 
 
 def _multiples_of_8(width, hidden):
-    if not (width > 0 and hidden > 0 and width % 8 == 0 and hidden % 8 == 0):
+    if width <= 0 or hidden <= 0 or width % 8 or hidden % 8:
         raise ValueError("width and hidden width: multiples of 8")
 
 
 def _rows_of_16_bytes(**tensors):
     for name, t in tensors.items():
-        if not (t.data_ptr() % 16 == 0 and _matrix_stride(t) % 8 == 0):
+        if t.data_ptr() % 16 or _matrix_stride(t) % 8:
             raise ValueError(f"{name}: its rows have to begin at multiples of 16 bytes")
 
 
 def _activation(name):
-    if not (name in _ACTIVATIONS):
+    if name not in _ACTIVATIONS:
         raise ValueError(f"activation: one of {sorted(_ACTIVATIONS)}")
     return _ACTIVATIONS[name]
+
+
+def _kept_views(room, tokens, hidden, dtype):
+    """The memory that a feed-forward block keeps, as the B item leaves it: d_pre and hidden."""
+    both = room.view(dtype)
+    n = 2 * tokens * hidden
+    return dict(pre=both[:n].view(tokens, 2 * hidden), hidden=both[n:].view(tokens, hidden))
+
+
+def _kept_memory(kept, tokens, hidden, dtype, device):
+    pre, h = kept["pre"], kept["hidden"]
+    _tensor(pre, "kept", device, (tokens, 2 * hidden), (dtype,))
+    _tensor(h, "kept", device, (tokens, hidden), (dtype,))
+    if h.untyped_storage().data_ptr() != pre.untyped_storage().data_ptr() or h.data_ptr() != pre.data_ptr() + 4 * tokens * hidden:
+        raise ValueError("kept: not the memory that gated_ffn returned")
+    return pre
 
 
 def gated_ffn(x, w_in, w_out, activation: str = "silu", keep: bool = False, out=None, workspace=None, stream=None):
     """(act(x w_gate^T) * (x w_up^T)) w_out^T, with w_in = [w_gate; w_up].  x: [tokens][width], rows any distance apart; w_in: [2
     hidden][width]; w_out: [width][hidden]; bfloat16 or float16; widths multiples of 8.  Returns dict(out, kept: with ``keep``,
-    what the two gradients need)."""
+    what the two gradients need, six bytes for each token and hidden channel)."""
     device = _device(x, "x")
     tokens, width, hidden = _ffn_sizes(x, "x", w_in, w_out, device)
     act = _activation(activation)
@@ -306,48 +322,45 @@ def gated_ffn(x, w_in, w_out, activation: str = "silu", keep: bool = False, out=
         else:
             _tensor(out, "out", device, (tokens, width), (x.dtype,), rows=True)
         _rows_of_16_bytes(x=x, w_in=w_in, w_out=w_out, out=out)
-        pre = s.empty(tokens, 2 * hidden, dtype=x.dtype) if keep else None
+        kept = s.empty(6 * tokens * hidden, dtype=torch.uint8) if keep else None
         h = s.empty(tokens, hidden, dtype=x.dtype)
         room = s.room(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
-        s.call("ffn", _TYPES[x.dtype], act, tokens, width, hidden, x.data_ptr(), _matrix_stride(x), w_in.data_ptr(), w_out.data_ptr(), _ptr(pre),
+        s.call("ffn", _TYPES[x.dtype], act, tokens, width, hidden, x.data_ptr(), _matrix_stride(x), w_in.data_ptr(), w_out.data_ptr(), _ptr(kept),
                h.data_ptr(), out.data_ptr(), _matrix_stride(out), *room)
-    return dict(out=out, **({"kept": dict(pre=pre, hidden=h)} if keep else {}))
+    return dict(out=out, **({"kept": _kept_views(kept, tokens, hidden, x.dtype)} if keep else {}))
 
 
 def gated_ffn_input_grad(grad, w_in, w_out, kept, activation: str = "silu", workspace=None, stream=None):
     """The B item: the gradient of x from that of the output and what ``gated_ffn`` kept.  Returns dict(x, kept: what
-    ``gated_ffn_weight_grad`` needs)."""
+    ``gated_ffn_weight_grad`` needs).  It takes the place of what was kept: this is called once for each ``gated_ffn``."""
     device = _device(grad, "grad")
     tokens, width, hidden = _ffn_sizes(grad, "grad", w_in, w_out, device)
     act = _activation(activation)
-    pre = _tensor(kept["pre"], "kept", device, (tokens, 2 * hidden), (grad.dtype,))
-    _rows_of_16_bytes(grad=grad, w_in=w_in, w_out=w_out, kept=pre)
+    memory = _kept_memory(kept, tokens, hidden, grad.dtype, device)
+    _rows_of_16_bytes(grad=grad, w_in=w_in, w_out=w_out, kept=memory)
     with _Stream(stream, device) as s:
         d_x = s.empty(tokens, width, dtype=grad.dtype)
-        d_pre = s.empty(tokens, 2 * hidden, dtype=grad.dtype)
         room = s.room(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
         s.call("ffn_input_grad", _TYPES[grad.dtype], act, tokens, width, hidden, grad.data_ptr(), _matrix_stride(grad), w_in.data_ptr(),
-               w_out.data_ptr(), pre.data_ptr(), d_pre.data_ptr(), d_x.data_ptr(), width, *room)
-    return dict(x=d_x, kept=dict(pre=d_pre))
+               w_out.data_ptr(), memory.data_ptr(), d_x.data_ptr(), width, *room)
+    return dict(x=d_x, kept=dict(pre=kept["pre"], hidden=kept["hidden"]))
 
 
 def gated_ffn_weight_grad(x, grad, kept, grad_kept, out=None, accumulate: bool = False, workspace=None, stream=None):
     """The W item: the weights' gradients from x, the output's gradient, what ``gated_ffn`` kept and what ``gated_ffn_input_grad``
-    kept.  out: dict(w_in, w_out) of tensors of x's type or, both, float32; accumulate: added to float32 ones.  Returns them."""
+    made of it.  out: dict(w_in, w_out) of tensors of x's type or, both, float32; accumulate: added to float32 ones.  Returns them."""
     device = _device(x, "x")
-    if not (x.dim() == 2):
+    if x.dim() != 2:
         raise ValueError("x: [tokens][width]")
     tokens, width = x.shape
     _tensor(x, "x", device, dtypes=_HALVES, rows=True)
     _tensor(grad, "grad", device, (tokens, width), (x.dtype,), rows=True)
-    h = kept["hidden"]
-    if not (h.dim() == 2):
-        raise ValueError("kept: of another call")
-    hidden = h.shape[1]
+    hidden = kept["hidden"].shape[-1]
     _multiples_of_8(width, hidden)
-    _tensor(h, "kept", device, (tokens, hidden), (x.dtype,))
-    d_pre = _tensor(grad_kept["pre"], "grad_kept", device, (tokens, 2 * hidden), (x.dtype,))
-    if not (not accumulate or out is not None and out["w_in"].dtype == torch.float32):
+    memory = _kept_memory(grad_kept, tokens, hidden, x.dtype, device)
+    if kept["pre"].data_ptr() != memory.data_ptr():
+        raise ValueError("grad_kept: of another call than kept")
+    if accumulate and (out is None or out["w_in"].dtype != torch.float32):
         raise ValueError("accumulate: needs float32 outputs")
     with _Stream(stream, device) as s:
         if out is None:
@@ -355,10 +368,10 @@ def gated_ffn_weight_grad(x, grad, kept, grad_kept, out=None, accumulate: bool =
         kind = out["w_in"].dtype
         _tensor(out["w_in"], "out", device, (2 * hidden, width), (x.dtype, torch.float32))
         _tensor(out["w_out"], "out", device, (width, hidden), (kind,))
-        _rows_of_16_bytes(x=x, grad=grad, kept=h, grad_kept=d_pre, w_in=out["w_in"], w_out=out["w_out"])
+        _rows_of_16_bytes(x=x, grad=grad, kept=memory, w_in=out["w_in"], w_out=out["w_out"])
         room = s.room(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
         s.call("ffn_weight_grad", _TYPES[x.dtype], tokens, width, hidden, x.data_ptr(), _matrix_stride(x), grad.data_ptr(), _matrix_stride(grad),
-               h.data_ptr(), d_pre.data_ptr(), _TYPES[kind], out["w_in"].data_ptr(), out["w_out"].data_ptr(), int(accumulate), *room)
+               memory.data_ptr(), _TYPES[kind], out["w_in"].data_ptr(), out["w_out"].data_ptr(), int(accumulate), *room)
     return out
 
 
@@ -371,13 +384,13 @@ def token_logprobs(logits, tokens, alternatives: int = 0, workspace=None, stream
     lowest id first, as ids: int32 [rows][k] and logprobs: float32 [rows][k]; -1 and -inf where fewer are not masked).  A logit of
     -inf is masked; a row with nothing else has logprob -inf and entropy 0; one with NaN or +inf is NaN throughout."""
     device = _device(logits, "logits")
-    if not (logits.dim() == 2 and logits.shape[1] > 0):
+    if logits.dim() != 2 or not logits.shape[1]:
         raise ValueError("logits: [rows][vocab]")
     n, vocab = logits.shape
     _tensor(logits, "logits", device, dtypes=_TYPES, rows=True)
     wide = _tokens(tokens, "tokens", device, (n,))
     k = int(alternatives)
-    if not (0 <= k <= MAX_ALTERNATIVES):
+    if not 0 <= k <= MAX_ALTERNATIVES:
         raise ValueError(f"alternatives: 0 to {MAX_ALTERNATIVES}")
     with _Stream(stream, device) as s:
         done = dict(logprob=s.empty(n, dtype=torch.float32), entropy=s.empty(n, dtype=torch.float32), lse=s.empty(n, 2, dtype=torch.float32))
@@ -394,7 +407,7 @@ def token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, grad_en
     """The gradient of the logits from those of ``logprob`` and ``entropy`` (float32 [rows], None: zero) and what ``token_logprobs``
     returned.  out: of the logits' type, may be ``logits`` itself.  Returns it."""
     device = _device(logits, "logits")
-    if not (logits.dim() == 2 and logits.shape[1] > 0):
+    if logits.dim() != 2 or not logits.shape[1]:
         raise ValueError("logits: [rows][vocab]")
     n, vocab = logits.shape
     _tensor(logits, "logits", device, dtypes=_TYPES, rows=True)

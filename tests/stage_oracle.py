@@ -142,7 +142,8 @@ def activation(g, name):
 
 
 def ffn(x, w_in, w_out, name, grad=None):
-    """dict of (value, bound) for out, x, w_in, w_out: the operator rounds hidden, and for the gradients g, u and d_pre, to the type."""
+    """dict of (value, bound) for out, x, w_in, w_out: the operator rounds hidden, and for the gradients d_pre, to the type, and keeps g and u in 24 bits
+    (15 behind the first: off by 2^-16 at most)."""
     dtype = x.dtype
     hidden = w_in.shape[0] // 2
     x, w_in, w_out = x.double(), w_in.double(), w_out.double()
@@ -158,11 +159,10 @@ def ffn(x, w_in, w_out, name, grad=None):
     found = dict(out=(y, rounded(y, y_e, dtype)))
     if grad is None:
         return found
-    r = HALF_STEP[dtype]
     d_y = grad.double()
     d_h, d_h_e = _product(d_y, w_out)
     # from g and u as kept
-    gk_e, uk_e = rounded(g, g_e, dtype), rounded(u, u_e, dtype)
+    gk_e, uk_e = (e + 2.0 ** -16 * (v.abs() + e) for v, e in ((g, g_e), (u, u_e)))
     slope_e = bend * gk_e + 40 * U + (0.0 if name != "relu" else (g.abs() <= gk_e).double())
     actk_e = steep * gk_e + 40 * U * (g.abs() + 1)
     def three(a, a_e, b, b_e, c, c_e):
@@ -172,7 +172,7 @@ def ffn(x, w_in, w_out, name, grad=None):
     d_g_e, d_u_e = three(d_h, d_h_e, u, uk_e, slope, slope_e), three(d_h, d_h_e, act, actk_e, one, zero)
     d_pre = torch.cat([d_g, d_u], 1)
     d_pre_e = rounded(d_pre, torch.cat([d_g_e, d_u_e], 1), dtype)
-    assert r > 0
+    h_e = rounded(h, actk_e * u.abs() + act.abs() * uk_e + actk_e * uk_e + U * h.abs(), dtype)   # (of the hidden made again from them)
     for key, (value, bound) in dict(x=_product(d_pre, w_in, d_pre_e), w_in=_product(d_pre.t(), x, d_pre_e.t()),
                                     w_out=_product(d_y.t(), h, None, h_e)).items():
         found[key] = (value, bound)   # (the caller rounds to the output's type)

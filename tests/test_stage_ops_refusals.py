@@ -85,10 +85,10 @@ def test_recurrence_pointers_and_workspace(lib):
     assert called(lib.fpsched_op_recurrence_grad, on, bytes=64) == ENOMEM
 
 
-FFN = dict(device=-1, type=0, act=0, tokens=20, width=64, hidden=128, x=P, x_stride=64, w_in=P, w_out=P, pre=P, h=P, out=P, out_stride=64, workspace=P, bytes=1 << 30, stream=None)
-FFN_B = dict(device=-1, type=0, act=0, tokens=20, width=64, hidden=128, grad=P, grad_stride=64, w_in=P, w_out=P, pre=P, d_pre=P, d_x=P, d_x_stride=64, workspace=P,
+FFN = dict(device=-1, type=0, act=0, tokens=20, width=64, hidden=128, x=P, x_stride=64, w_in=P, w_out=P, kept=P, h=P, out=P, out_stride=64, workspace=P, bytes=1 << 30, stream=None)
+FFN_B = dict(device=-1, type=0, act=0, tokens=20, width=64, hidden=128, grad=P, grad_stride=64, w_in=P, w_out=P, kept=P, d_x=P, d_x_stride=64, workspace=P,
              bytes=1 << 30, stream=None)
-FFN_W = dict(device=-1, type=0, tokens=20, width=64, hidden=128, x=P, x_stride=64, grad=P, grad_stride=64, h=P, d_pre=P, out_type=2, d_w_in=P, d_w_out=P, accumulate=0,
+FFN_W = dict(device=-1, type=0, tokens=20, width=64, hidden=128, x=P, x_stride=64, grad=P, grad_stride=64, kept=P, out_type=2, d_w_in=P, d_w_out=P, accumulate=0,
              workspace=P, bytes=1 << 30, stream=None)
 
 
@@ -102,7 +102,7 @@ def test_ffn(lib, name, defaults):
     for change in changes:
         assert called(f, defaults, **change) == EINVAL, change
     on = dict(defaults, device=0)
-    pointers = [key for key in defaults if defaults[key] == P and key not in ("workspace", "pre")]
+    pointers = [key for key in defaults if defaults[key] == P and key != "workspace" and not (key == "kept" and name == "ffn")]
     for change in [{key: bad} for key in pointers for bad in (None, P + 8)] + [{key: 68} for key in defaults if key.endswith("stride")]:
         assert called(f, on, **change) == EINVAL, change
 
@@ -155,7 +155,8 @@ def test_python_functions_check_their_tensors():
                  lambda: ops.gated_recurrence_grad(x[None], x[None], x[None], zeros(1, 2, 64, dtype=f)),
                  lambda: ops.gated_ffn(x, w_in, w_out, "tanh"), lambda: ops.gated_ffn(x.float(), w_in.float(), w_out.float()), lambda: ops.gated_ffn(x, w_in, w_out.t()),
                  lambda: ops.gated_ffn(x, w_in[:63], w_out), lambda: ops.gated_ffn(zeros(4, 65)[:, 1:], w_in, w_out), lambda: ops.gated_ffn(x[:, :60], w_in[:, :60].contiguous(), w_out[:60]),
-                 lambda: ops.gated_ffn_input_grad(x, w_in, w_out, dict(pre=zeros(4, 60))), lambda: ops.gated_ffn_weight_grad(x, x, dict(hidden=zeros(4, 32)), dict(pre=zeros(4, 32))),
+                 lambda: ops.gated_ffn_input_grad(x, w_in, w_out, dict(pre=zeros(4, 60), hidden=zeros(4, 30))), lambda: ops.gated_ffn_input_grad(x, w_in, w_out, dict(pre=zeros(4, 64), hidden=zeros(4, 32))),
+                 lambda: ops.gated_ffn_weight_grad(x, x, dict(pre=zeros(4, 64), hidden=zeros(4, 32)), dict(pre=zeros(4, 64), hidden=zeros(4, 32))),
                  lambda: ops.token_logprobs(x, tokens, 33), lambda: ops.token_logprobs(x, tokens[:2]), lambda: ops.token_logprobs(x[0], tokens),
                  lambda: ops.token_logprobs_grad(x, tokens, zeros(4, dtype=f), zeros(4, dtype=f)),
                  lambda: ops.token_logprobs(x, tokens, workspace=torch.zeros(100, dtype=torch.uint8))):
