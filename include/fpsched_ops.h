@@ -89,7 +89,7 @@ int fpsched_op_recurrence_grad(int device_id, int type, int64_t n_batch, int64_t
  * FPSCHED_FFN_KEPT_BYTES of g and u in 24 bits for the backward pass.  Types FPSCHED_BF16 and FPSCHED_F16, the
  * same for all; weights and hidden contiguous.  width, hidden_width and the strides are multiples of 8,
  * the tensors 16-byte aligned (FPSCHED_EINVAL): rows are moved 16 bytes at a time.  act is computed in 32
- * bits from unrounded g and u. */
+ * bits from unrounded g and u.  FPSCHED_EUNSUPPORTED where a product has 2^23 tiles of 128 x 128 or more. */
 enum { FPSCHED_SILU = 0, FPSCHED_GELU = 1 /* with tanh */, FPSCHED_RELU = 2 };
 #define FPSCHED_FFN_KEPT_BYTES(n_tokens, hidden_width) ((size_t)6 * (n_tokens) * (hidden_width))
 size_t fpsched_op_ffn_workspace_bytes(int64_t n_tokens, int64_t width, int64_t hidden_width);

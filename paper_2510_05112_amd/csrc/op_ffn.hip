@@ -36,7 +36,7 @@ struct Frag<_Float16> {
 };
 
 enum { kAlong, kDown };                        // how k lies in an operand
-enum { kStore, kGated, kGatedGrad, kPart };    // what becomes of a tile
+enum { kStore, kGated, kGatedGrad };           // what becomes of a tile
 constexpr int kDepth = 64;                     // k of a tile in LDS
 constexpr unsigned kOutside = 0x80000000u;     // an offset behind the end of every tile's buffer
 
@@ -56,7 +56,9 @@ struct Gemm {
   int act;
   void* kept;                // kGated: written unless NULL; kGatedGrad: read, and written in its place
   int tiles_m, tiles_n;
-  int64_t part_depth;        // kPart: a part's k
+  int whole, parts;          // tiles that one workgroup each works on; of the others, workgroups that share k
+  int64_t part_depth;        // a share of k
+  float* sums;               // their sums: [tile - whole][part][row][column]
 };
 
 // ---- activations: the value, and with it the derivative ----------------------------------------------------------------
@@ -292,13 +294,18 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
   const int thread = threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int wave_m = wave / kWavesN, wave_n = wave % kWavesN;
   int tm, tn;
-  tile_of(blockIdx.x, a.tiles_m, a.tiles_n, &tm, &tn);
-  if constexpr (EPILOGUE == kPart) {   // blockIdx.y: a part of k, whose sums have a place of their own
-    const int64_t k0 = (int64_t)blockIdx.y * a.part_depth;
+  const bool shared = (int)blockIdx.x >= a.whole;
+  float* sums = nullptr;
+  if (shared) {
+    const int of = blockIdx.x - a.whole, part = of % a.parts;
+    tile_of(a.whole + of / a.parts, a.tiles_m, a.tiles_n, &tm, &tn);
+    sums = a.sums + (int64_t)of * BM * BN;
+    const int64_t k0 = part * a.part_depth;
     a.m.data = static_cast<const T*>(a.m.data) + k0 * (LM == kAlong ? 1 : a.m.stride);
     a.n.data = static_cast<const T*>(a.n.data) + k0 * (LN == kAlong ? 1 : a.n.stride);
     a.depth = min(a.part_depth, a.depth - k0);
-    a.out = static_cast<float*>(a.out) + blockIdx.y * a.m.extent * a.out_stride;
+  } else {
+    tile_of(blockIdx.x, a.tiles_m, a.tiles_n, &tm, &tn);
   }
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * (kHalves ? BN / 2 : BN);
   f32x16 acc[MF][NF] = {};
@@ -377,6 +384,17 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
       const int r = p * kRows + lane / kLanes;
       const int64_t m = rows + r;
       const float* from = mine + r * kPad + lane % kLanes * 8;
+      if (shared) {   // (a tile's own rows and columns, the other half's behind the gate's)
+        if (m >= a.m.extent) continue;
+        float* to = sums + ((wave_m * MF + i) * 32 + r) * BN + wave_n * kColumns + lane % kLanes * 8;
+        store_vec<float, 4>(to, load_vec<float, 4>(from));
+        store_vec<float, 4>(to + 4, load_vec<float, 4>(from + 4));
+        if constexpr (kHalves) {
+          store_vec<float, 4>(to + BN / 2, load_vec<float, 4>(from + kColumns));
+          store_vec<float, 4>(to + BN / 2 + 4, load_vec<float, 4>(from + kColumns + 4));
+        }
+        continue;
+      }
       const Vec<float, 4> x0 = load_vec<float, 4>(from), x1 = load_vec<float, 4>(from + 4);
       if constexpr (kHalves) {
         const Vec<float, 4> u0 = load_vec<float, 4>(from + kColumns), u1 = load_vec<float, 4>(from + kColumns + 4);
@@ -485,79 +503,89 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(O* out, int64_t stride, 
     out[i / columns * stride + i % columns] = (O)0.f;
 }
 
-// The parts of a product added up in order, and what becomes of it.
-template <typename T, int EPILOGUE, typename O>
-__global__ __launch_bounds__(256) void add_parts_kernel(Gemm a, const float* parts, int n_parts) {
-  const int64_t columns = a.n.extent, pieces = (EPILOGUE == kGated ? a.n_half : columns) / 8;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, m = at / pieces, n = at % pieces * 8;
-  if (m >= a.m.extent) return;
-  auto total = [&](int64_t from) {
+// The sums of the workgroups that share a tile, added up in order, and what becomes of them.
+template <typename T, int EPILOGUE, typename O, int SIDE>
+__global__ __launch_bounds__(256) void add_shares_kernel(Gemm a) {
+  constexpr int kColumns = EPILOGUE == kGated ? SIDE / 2 : SIDE, kPieces = kColumns / 8, kGroups = SIDE * kPieces / 256;
+  const int tile = blockIdx.x / kGroups, at = blockIdx.x % kGroups * 256 + threadIdx.x, r = at / kPieces, c = at % kPieces * 8;
+  int tm, tn;
+  tile_of(a.whole + tile, a.tiles_m, a.tiles_n, &tm, &tn);
+  const int64_t m = (int64_t)tm * SIDE + r, n = (int64_t)tn * kColumns + c;
+  if (m >= a.m.extent || n >= (EPILOGUE == kGated ? a.n_half : a.n.extent)) return;
+  auto total = [&](int column) {
     Vec<float, 8> sum = {};
-    for (int p = 0; p < n_parts; ++p) {
-      const float* x = parts + (p * a.m.extent + m) * columns + from;
+    const float* x = a.sums + ((int64_t)tile * a.parts * SIDE + r) * SIDE + column;
+    for (int p = 0; p < a.parts; ++p, x += SIDE * SIDE) {
       const Vec<float, 4> low = load_vec<float, 4>(x), high = load_vec<float, 4>(x + 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum.at[e] += low.at[e], sum.at[e + 4] += high.at[e];
     }
     return sum;
   };
-  if constexpr (EPILOGUE == kGated) put_gated<T, 8>(a, m, n, total(n), total(a.n_half + n));
-  else put_columns<T, EPILOGUE, O>(a, m, n, total(n));
+  if constexpr (EPILOGUE == kGated) put_gated<T, 8>(a, m, n, total(c), total(SIDE / 2 + c));
+  else put_columns<T, EPILOGUE, O>(a, m, n, total(c));
 }
 
-// How a product is cut.  Tiles of 256 x 256 where there are enough of them to go round the compute units, else of 128 x 128, two workgroups
-// to a compute unit; where even of those there are few, k is cut into parts, whose sums are added up by another kernel.  What decides is an
-// estimate: a tile's step of 64 k takes 0.65 us with one workgroup to a compute unit and 1.1 with two; the parts are
-// written and read at 8 TB/s, in a launch more.
+// How a product is cut: into tiles of 256 x 256, one workgroup to a compute unit, or of 128 x 128, two of them; and the tiles
+// of the last round, where they leave compute units idle, into shares of k, whose sums another kernel adds up.  What decides is an estimate:
+// a step of 64 k takes 1.63 us and what becomes of a tile 5 (of the gate's gradient 30, which is 0.8 MB a tile); of the small tiles 1.1 us, 0.65 with one workgroup to a compute
+// unit, and 3; sums are written and read at 8 TB/s, in a launch more.  (Measured: 1,344 tiles of 128 steps, five rounds and a quarter, 1.25 ms whole and 1.13
+// with the last quarter in four shares; 80 small tiles of 216 steps 134 us whole and 30 in six.)
 struct Split {
   bool large;
-  int parts;
+  int tiles_m, tiles_n, whole, parts;
   int64_t part_depth;
 };
 
-Split split(int64_t m, int64_t n, int64_t depth) {
-  Split s{ceil_div(m, 256) * ceil_div(n, 256) >= 160, 1, depth};
-  if (s.large) return s;
-  const int64_t tiles = ceil_div(m, 128) * ceil_div(n, 128), steps = ceil_div(depth, kDepth);
-  double best = 0;
-  for (int parts = 1; parts <= 16 && steps >= 4 * parts; ++parts) {
-    const int64_t each = ceil_div(steps, parts), groups = tiles * parts;
-    const double us = each * (groups <= 256 ? 0.65 : 1.1 * ceil_div(groups, 512)) + (parts > 1 ? 4 + parts * (m * n * 8 / 8e6) : 0);
-    if (parts == 1 || us < best) {
-      best = us;
-      s.parts = (int)ceil_div(steps, each);
-      s.part_depth = s.parts == 1 ? depth : each * kDepth;
+Split split(int64_t m, int64_t n, int64_t depth, bool heavy) {
+  Split best = {};
+  double least = 0;
+  const int64_t steps = ceil_div(depth, kDepth);
+  for (const bool large : {true, false}) {
+    const int64_t side = large ? 256 : 128, slots = large ? 256 : 512, tm = ceil_div(m, side), tn = ceil_div(n, side), tiles = tm * tn;
+    if (large && tiles < 64) continue;
+    const double step = large ? 1.63 : 1.1, end = (large ? 5 : 3) * (heavy ? 6 : 1);
+    const int64_t rounds = tiles / slots, rest = tiles % slots;
+    for (int parts = 1; parts <= 16 && (parts == 1 || (rest && steps >= 4 * parts)); ++parts) {
+      const int64_t each = ceil_div(steps, parts), used = ceil_div(steps, each);   // (as many shares as there is something for)
+      const double alone = !large && rounds == 0 && rest * used <= 256 ? 0.65 : step;
+      const double us = rounds * (steps * step + end) + (rest ? ceil_div(rest * used, slots) * (each * alone + (used > 1 ? 3 : end)) : 0) +
+                        (used > 1 ? 4 + end + rest * used * (std::min(m, side) * side * 8 / 8e6) : 0);
+      if (least == 0 || us < least) {
+        least = us;
+        best = {large, (int)std::min<int64_t>(tm, INT32_MAX), (int)std::min<int64_t>(tn, INT32_MAX), (int)std::min<int64_t>(used > 1 ? tiles - rest : tiles, INT32_MAX), (int)used, each * kDepth};
+      }
     }
   }
-  return s;
+  return best;
 }
 
-size_t split_bytes(int64_t m, int64_t n, int64_t depth) {
-  const Split s = split(m, n, depth);
-  return s.parts > 1 ? (size_t)s.parts * m * n * sizeof(float) : 0;
+size_t split_bytes(int64_t m, int64_t n, int64_t depth, bool heavy) {
+  const Split s = split(m, n, depth, heavy);
+  const size_t side = s.large ? 256 : 128;
+  return s.parts > 1 ? ((size_t)s.tiles_m * s.tiles_n - s.whole) * s.parts * side * side * sizeof(float) : 0;
 }
 
 template <typename T, int LM, int LN, int EPILOGUE, typename O>
 int gemm(Gemm a, void* workspace, hipStream_t stream) {
-  const int64_t columns = a.n.extent;   // (of kGated: both halves)
-  const Split s = split(a.m.extent, columns, a.depth);
-  const int64_t side = s.large ? 256 : 128, tm = ceil_div(a.m.extent, side), tn = ceil_div(columns, side);
-  if (tm * tn > 0x7fffffff) return FPSCHED_EINVAL;
-  a.tiles_m = (int)tm;
-  a.tiles_n = (int)tn;
+  const Split s = split(a.m.extent, a.n.extent, a.depth, EPILOGUE == kGatedGrad);   // (of kGated, n has both halves)
+  const int64_t tiles = (int64_t)s.tiles_m * s.tiles_n;
+  if (tiles > 0x7fffff) return FPSCHED_EUNSUPPORTED;   // (workgroups and their numbers are 32-bit)
+  a.tiles_m = s.tiles_m;
+  a.tiles_n = s.tiles_n;
+  a.whole = s.whole;
+  a.parts = s.parts;
+  a.part_depth = s.part_depth;
+  a.sums = static_cast<float*>(workspace);
+  const int shared = (int)(tiles - s.whole);
+  const dim3 grid(s.whole + shared * s.parts);
+  constexpr int kHalf = EPILOGUE == kGated ? 2 : 1;
   if (s.large) {
-    gemm_kernel<T, LM, LN, EPILOGUE, O, 256, 256, 2, 4><<<dim3((unsigned)(tm * tn)), dim3(512), 0, stream>>>(a);
-  } else if (s.parts == 1) {
-    gemm_kernel<T, LM, LN, EPILOGUE, O, 128, 128, 2, 2><<<dim3((unsigned)(tm * tn)), dim3(256), 0, stream>>>(a);
+    gemm_kernel<T, LM, LN, EPILOGUE, O, 256, 256, 2, 4><<<grid, dim3(512), 0, stream>>>(a);
+    if (shared) add_shares_kernel<T, EPILOGUE, O, 256><<<dim3(shared * 32 / kHalf), dim3(256), 0, stream>>>(a);
   } else {
-    Gemm part = a;
-    part.out = workspace;
-    part.out_stride = columns;
-    part.part_depth = s.part_depth;
-    part.accumulate = 0;
-    gemm_kernel<T, LM, LN, kPart, float, 128, 128, 2, 2><<<dim3((unsigned)(tm * tn), s.parts), dim3(256), 0, stream>>>(part);
-    const int64_t pieces = a.m.extent * ((EPILOGUE == kGated ? a.n_half : columns) / 8);
-    add_parts_kernel<T, EPILOGUE, O><<<dim3((unsigned)ceil_div(pieces, 256)), dim3(256), 0, stream>>>(a, static_cast<const float*>(workspace), s.parts);
+    gemm_kernel<T, LM, LN, EPILOGUE, O, 128, 128, 2, 2><<<grid, dim3(256), 0, stream>>>(a);
+    if (shared) add_shares_kernel<T, EPILOGUE, O, 128><<<dim3(shared * 8 / kHalf), dim3(256), 0, stream>>>(a);
   }
   return launched();
 }
@@ -576,8 +604,9 @@ int check_sizes(int type, int act, int64_t n_tokens, int64_t width, int64_t hidd
 // Room for the largest of the products' parts.
 size_t workspace_for(int64_t t, int64_t k, int64_t f) {
   if (t == 0) return 16;
-  const size_t forward = t <= kFewRows ? 0 : std::max(split_bytes(t, 2 * f, k), split_bytes(t, k, f));
-  const size_t backward = std::max(split_bytes(t, f, k), split_bytes(t, k, 2 * f)), weights = std::max(split_bytes(2 * f, k, t), split_bytes(k, f, t));
+  const size_t forward = t <= kFewRows ? 0 : std::max(split_bytes(t, 2 * f, k, false), split_bytes(t, k, f, false));
+  const size_t backward = std::max(split_bytes(t, f, k, true), split_bytes(t, k, 2 * f, false));
+  const size_t weights = std::max(split_bytes(2 * f, k, t, false), split_bytes(k, f, t, false));
   return std::max<size_t>({16, forward, backward, weights});
 }
 
