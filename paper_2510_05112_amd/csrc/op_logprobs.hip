@@ -6,9 +6,9 @@
 // bytes of logits at a time and changes its m only where one of them is larger.  Rows are cut into parts where there are fewer rows than
 // the chip has room for; a second kernel puts the parts together.
 //
-// Alternatives: the lanes keep their logits of the part in registers.  The k-th largest of a wavefront's lanes' largest logits has k logits at
-// least that are not below it; those of the whole part that are not below the highest of the wavefronts' such bars are
-// collected in LDS (about k of them), and each finds its place by counting the larger ones.  Equal logits come by ascending id: a candidate is
+// Alternatives: the lanes keep their logits of the part in registers.  Of 32 groups of lanes each has a largest logit, and k logits at least are
+// not below the k-th of these; those that are not are collected in LDS (little more than k of them),
+// and each finds its place by counting the larger ones.  Equal logits come by ascending id: a candidate is
 // the logit's bits, in an order in which they compare as integers, with the id behind.  Where too many are equal to the bar (a row of one value) the k are found one by one.
 //
 // Masked logits are minus infinity, and x - m = -infinity gives e = 0, but 0 times it is NaN: factors are held at -1000.  m begins at the
@@ -55,18 +55,34 @@ struct Stats {
 
 __device__ __forceinline__ Stats nothing() { return {-FLT_MAX, 0.f, 0.f}; }
 
+// The value of the lane across: of steps 1, 2, 4, ... in turn, where the values of each group of STEP lanes are the same already, lanes of the
+// other group of STEP.
+template <int STEP>
+__device__ __forceinline__ float across(float x) {
+  const int i = __float_as_int(x);
+  if constexpr (STEP == 1) return __int_as_float(__builtin_amdgcn_update_dpp(i, i, 0xb1, 0xf, 0xf, false));        // neighbours in pairs
+  else if constexpr (STEP == 2) return __int_as_float(__builtin_amdgcn_update_dpp(i, i, 0x4e, 0xf, 0xf, false));   // pairs in fours
+  else if constexpr (STEP == 4) return __int_as_float(__builtin_amdgcn_update_dpp(i, i, 0x141, 0xf, 0xf, false));  // eights mirrored
+  else if constexpr (STEP == 8) return __int_as_float(__builtin_amdgcn_update_dpp(i, i, 0x140, 0xf, 0xf, false));  // sixteens mirrored
+  else if constexpr (STEP == 16) return __int_as_float(__builtin_amdgcn_ds_swizzle(i, 0x401f));
+  else return __shfl_xor(x, 32);
+}
+template <typename F>
+__device__ __forceinline__ float over_lanes(float x, F f) {
+  x = f(x, across<1>(x));
+  x = f(x, across<2>(x));
+  x = f(x, across<4>(x));
+  x = f(x, across<8>(x));
+  x = f(x, across<16>(x));
+  return f(x, across<32>(x));
+}
 __device__ __forceinline__ Stats wave_stats(Stats a) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    Stats o;
-    o.m = __shfl_xor(a.m, d);
-    o.s = __shfl_xor(a.s, d);
-    o.w = __shfl_xor(a.w, d);
-    a.join(o);
-  }
+  auto add = [](float x, float y) { return x + y; };
+  a.raise(over_lanes(a.m, [](float x, float y) { return fmaxf(x, y); }));
+  a.s = over_lanes(a.s, add);
+  a.w = over_lanes(a.w, add);
   return a;
 }
-
 // A logit and its id as one number: larger for a larger logit, then for a smaller id.  0: none.
 __device__ __forceinline__ unsigned long long ranked(float x, unsigned id) {
   const unsigned bits = __float_as_uint(x), order = bits & 0x80000000u ? ~bits : bits | 0x80000000u;
@@ -85,6 +101,8 @@ __device__ __forceinline__ unsigned long long wave_most(unsigned long long a) {
   return a;
 }
 
+constexpr int kGroups = 8 * kWaves;   // of eight lanes
+static_assert(kMostAlternatives <= kGroups, "as many groups of lanes as alternatives");
 constexpr int kRoom = 512;   // candidates in LDS
 
 // put(place, candidate) if the at-th of n distinct candidates in LDS is one of the k largest.
@@ -143,11 +161,11 @@ struct RowOut {
 
 // One part of a row.  blockIdx.x: row * parts + part.  ALT: with alternatives, of at most kHeldPart logits.
 template <typename T, bool ALT>
-__global__ __launch_bounds__(kThreads, 4) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
   constexpr int N = kWide<T>;
   __shared__ Stats wave_sums[kWaves];
   __shared__ unsigned long long candidates[ALT ? kRoom : 1];
-  __shared__ float bars[kWaves];
+  __shared__ __align__(16) float group_tops[kGroups];
   __shared__ int collected;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = row_out.k;
   const int64_t row = blockIdx.x / part_out.parts, part = blockIdx.x % part_out.parts;
@@ -200,35 +218,36 @@ __global__ __launch_bounds__(kThreads, 4) void logprobs_kernel(RowOut<T> row_out
       for (int i = 0; i < kAhead; ++i) take(v[i]);
     }
   }
-  float bar = -INFINITY;
   if constexpr (ALT) {
-    // the lane's largest, and how many lanes' are larger (or as large, of lanes in front)
     float most = tops[0];
 #pragma unroll
     for (int p = 1; p < kPieces; ++p) most = fmaxf(most, tops[p]);
-    int larger = 0;
-#pragma unroll
-    for (int l = 0; l < 64; ++l) {
-      const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(most), l));
-      larger += other > most || (other == most && l < lane);
-    }
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {   // (what is looked at again is converted again: kept as 32-bit numbers it would take the registers of a wavefront)
       Vec<unsigned, 4> words = __builtin_bit_cast(Vec<unsigned, 4>, held[p]);
       asm volatile("" : "+v"(words.at[0]), "+v"(words.at[1]), "+v"(words.at[2]), "+v"(words.at[3]));
       held[p] = __builtin_bit_cast(Held, words);
     }
-    const unsigned long long at = __ballot(larger == k - 1);
-    bar = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(most), __builtin_ctzll(at)));
-    if (lane == 0) bars[wave] = bar;
+    most = fmaxf(most, across<1>(most));
+    most = fmaxf(most, across<2>(most));
+    most = fmaxf(most, across<4>(most));
+    if ((lane & 7) == 0) group_tops[wave * 8 + (lane >> 3)] = most;
     if (threadIdx.x == 0) collected = 0;
   }
   const Stats sums = wave_stats(mine);
   if (lane == 0) wave_sums[wave] = sums;
   __syncthreads();
   if constexpr (ALT) {
+    const float mine_of_groups = group_tops[lane & (kGroups - 1)];
+    int larger = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) bar = fmaxf(bar, bars[w]);
+    for (int g = 0; g < kGroups; g += 4) {
+      const Vec<float, 4> others = load_vec<float, 4>(group_tops + g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) larger += others.at[i] > mine_of_groups || (others.at[i] == mine_of_groups && g + i < (lane & (kGroups - 1)));
+    }
+    const unsigned long long at_bar = __ballot(larger == k - 1);
+    const float bar = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine_of_groups), __builtin_ctzll(at_bar)));
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
       if (tops[p] >= bar) {

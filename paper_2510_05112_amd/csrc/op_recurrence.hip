@@ -391,7 +391,8 @@ __global__ __launch_bounds__(kGradWaves * 64) void recurrence_grad_kernel(Recurr
 }
 
 // Segments of a sequence: enough for four workgroups a compute unit, and none where there are two each without (a segment's steps are read
-// twice).
+// twice).  65,536 steps of 2,560 forward, 4 x 1,021 of 4,096 in both directions: for two workgroups a compute unit 380 and 84 us, for four 347
+// and 78, for six 368 and 78.
 struct Cut {
   int blocks, segment_blocks, segments;
 };
