@@ -161,7 +161,7 @@ struct RowOut {
 
 // One part of a row.  blockIdx.x: row * parts + part.  ALT: with alternatives, of at most kHeldPart logits.
 template <typename T, bool ALT>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 5) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
   constexpr int N = kWide<T>;
   __shared__ Stats wave_sums[kWaves];
   __shared__ unsigned long long candidates[ALT ? kRoom : 1];
