@@ -364,7 +364,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
     for (int j = 0; j < NF; ++j) acc[i][j] = Frag<T>::mul(fn[(kStepsOfTile - 1) & 1][j], fm[(kStepsOfTile - 1) & 1][i], acc[i][j]);
   // A wavefront's 32 rows at a time go through LDS, so that rows are read and written 8 columns a lane.
   constexpr int kPad = NF * 32 + 4;   // floats between rows: 16 rows' pieces of 16 bytes are in different banks
-  __syncthreads();
+  meet();   // (the loads of the tile behind the last one, zeros, among them)
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kPad;
   static_assert(kThreads / 64 * 32 * kPad * 4 <= 2 * kTile, "the rows fit");
 #pragma unroll
