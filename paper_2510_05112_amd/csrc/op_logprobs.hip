@@ -458,7 +458,9 @@ int fpsched_op_logprobs_grad(int device_id, int type, int64_t n_rows, int64_t vo
   if (type < FPSCHED_BF16 || type > FPSCHED_F32 || !sizes_fit(n_rows, vocab, 0) || logits_stride < vocab || out_stride < vocab) return FPSCHED_EINVAL;
   if (device_id < 0) return FPSCHED_ENODEV;
   if (n_rows == 0) return FPSCHED_OK;
+  const size_t element = type == FPSCHED_F32 ? 4 : 2;
   if (!logits || !tokens || !lse || !entropy || !out || (out == logits && out_stride != logits_stride)) return FPSCHED_EINVAL;
+  if (!aligned(logits, element) || !aligned(out, element)) return FPSCHED_EINVAL;
   OpsDevice g(device_id);
   if (!g.ok) return FPSCHED_EHIP;
   return with_type(type, [&](auto zero) {

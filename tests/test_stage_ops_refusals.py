@@ -126,7 +126,8 @@ def test_logprobs_pointers_and_workspace(lib):
     assert called(lib.fpsched_op_logprobs_grad, LOGPROBS_GRAD) == ENODEV
     for change in (dict(out_stride=49999), dict(stride=1), dict(type=3), dict(vocab=0)):
         assert called(lib.fpsched_op_logprobs_grad, LOGPROBS_GRAD, **change) == EINVAL, change
-    assert called(lib.fpsched_op_logprobs_grad, dict(LOGPROBS_GRAD, device=0), stride=50008) == EINVAL   # (in place, with another stride)
+    for change in (dict(stride=50008), dict(out=P + 1), dict(logits=P + 3), dict(lse=None), dict(out=None)):   # (the first: in place, with another stride)
+        assert called(lib.fpsched_op_logprobs_grad, dict(LOGPROBS_GRAD, device=0), **change) == EINVAL, change
 
 
 def test_python_functions_need_cuda_tensors():
