@@ -43,14 +43,6 @@ struct Stats {
     s += e;
     w += e * held_back(x - m);
   }
-  __device__ __forceinline__ void join(const Stats& o) {
-    const float most = fmaxf(m, o.m);
-    Stats other = o;
-    raise(most);
-    other.raise(most);
-    s += other.s;
-    w += other.w;
-  }
 };
 
 __device__ __forceinline__ Stats nothing() { return {-FLT_MAX, 0.f, 0.f}; }
@@ -76,6 +68,7 @@ __device__ __forceinline__ float over_lanes(float x, F f) {
   x = f(x, across<16>(x));
   return f(x, across<32>(x));
 }
+// The lanes' sums put together.
 __device__ __forceinline__ Stats wave_stats(Stats a) {
   auto add = [](float x, float y) { return x + y; };
   a.raise(over_lanes(a.m, [](float x, float y) { return fmaxf(x, y); }));
@@ -83,15 +76,28 @@ __device__ __forceinline__ Stats wave_stats(Stats a) {
   a.w = over_lanes(a.w, add);
   return a;
 }
+// The sums of kWaves wavefronts, by each lane.
+__device__ __forceinline__ Stats put_together(const Stats* wave_sums, int lane) {
+  static_assert(kWaves == 4, "the lanes are taken in fours");
+  Stats a = wave_sums[lane & 3];
+  float most = fmaxf(a.m, across<1>(a.m));
+  a.raise(fmaxf(most, across<2>(most)));
+  a.s += across<1>(a.s);
+  a.s += across<2>(a.s);
+  a.w += across<1>(a.w);
+  a.w += across<2>(a.w);
+  return a;
+}
+// A number that is larger for a larger x (not 0 for any that is a number).
+__device__ __forceinline__ unsigned in_order(float x) {
+  const unsigned bits = __float_as_uint(x);
+  return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+}
+__device__ __forceinline__ float out_of_order(unsigned order) { return __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order); }
+
 // A logit and its id as one number: larger for a larger logit, then for a smaller id.  0: none.
-__device__ __forceinline__ unsigned long long ranked(float x, unsigned id) {
-  const unsigned bits = __float_as_uint(x), order = bits & 0x80000000u ? ~bits : bits | 0x80000000u;
-  return (unsigned long long)order << 32 | (unsigned)~id;
-}
-__device__ __forceinline__ float logit_of(unsigned long long r) {
-  const unsigned order = (unsigned)(r >> 32);
-  return __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
-}
+__device__ __forceinline__ unsigned long long ranked(float x, unsigned id) { return (unsigned long long)in_order(x) << 32 | (unsigned)~id; }
+__device__ __forceinline__ float logit_of(unsigned long long r) { return out_of_order((unsigned)(r >> 32)); }
 __device__ __forceinline__ unsigned long long wave_most(unsigned long long a) {
 #pragma unroll
   for (int d = 32; d; d >>= 1) {
@@ -161,36 +167,38 @@ struct RowOut {
 
 // One part of a row.  blockIdx.x: row * parts + part.  ALT: with alternatives, of at most kHeldPart logits.
 template <typename T, bool ALT>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 5) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
   constexpr int N = kWide<T>;
   __shared__ Stats wave_sums[kWaves];
   __shared__ unsigned long long candidates[ALT ? kRoom : 1];
-  __shared__ __align__(16) float group_tops[kGroups];
+  __shared__ __align__(16) unsigned group_tops[kGroups];
   __shared__ int collected;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = row_out.k;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = row_out.k;
   const int64_t row = blockIdx.x / part_out.parts, part = blockIdx.x % part_out.parts;
   const T* logits = row_out.logits + row * row_out.stride;
   bool is_given = false;
   const float given = part_out.parts == 1 ? row_out.given(row, &is_given) : 0.f;   // (on its way while the row is read)
-  // pieces of 16 bytes that are aligned as such, the first and the last one cut off at the part's ends
+  // Pieces of 16 bytes that are aligned as such, from `inner` on, and up to N - 1 logits in front of them and behind them, one a lane.
   const int64_t begin = part * part_length, end = min(begin + part_length, row_out.vocab);
-  const int64_t skew = (int64_t)((reinterpret_cast<uintptr_t>(logits + begin) & 15) / sizeof(T));
-  Stats mine = nothing();
-  constexpr int kPieces = kHeld / N + 1;   // (a piece more, since the first begins in front of the part)
-  using Held = Vec<T, N>;
-  Held held[ALT ? kPieces : 1];
-  auto get = [&](int64_t at, T none) {     // logits at .. at + N - 1
+  const int64_t skew = (int64_t)((0 - reinterpret_cast<uintptr_t>(logits + begin)) % 16 / sizeof(T));
+  const int64_t inner = min(begin + skew, end);
+  const unsigned length = (unsigned)((end - inner) / N * N), mine_at = threadIdx.x * N;
+  const int64_t outer = threadIdx.x < N ? begin + threadIdx.x : inner + length + threadIdx.x - N;
+  const bool has_outer = threadIdx.x < N ? outer < inner : threadIdx.x < 2 * N && outer < end;
+  const float x_outer = has_outer ? (float)logits[outer] : -INFINITY;
+  auto get = [&](unsigned at) {
     Vec<T, N> v;
-    if (at >= begin && at + N <= end) {
-      v = load_vec<T, N>(logits + at);
+    if (at < length) {
+      v = load_vec<T, N>(logits + inner + at);
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) v.at[i] = at + i >= begin && at + i < end ? logits[at + i] : none;
+      for (int i = 0; i < N; ++i) v.at[i] = (T)-INFINITY;
     }
     return v;
   };
+  Stats mine = nothing();
   auto take = [&](const Vec<T, N>& v) {   // returns the largest
-    float x[N], most = -FLT_MAX;
+    float x[N], most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       x[i] = (float)v.at[i];
@@ -201,75 +209,74 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 5) void logprobs_ker
     for (int i = 0; i < N; ++i) mine.add(x[i]);
     return most;
   };
-  float tops[ALT ? kPieces : 1];   // of the pieces held
-  const int64_t first = begin - skew + (int64_t)threadIdx.x * N;
+  constexpr int kPieces = kHeld / N;
+  float tops[ALT ? kPieces : 1];   // the pieces' largest logits
   if constexpr (ALT) {
+    Vec<T, N> v[kPieces];
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) held[p] = get(first + (int64_t)p * kThreads * N, (T)-INFINITY);
+    for (int p = 0; p < kPieces; ++p) v[p] = get(mine_at + p * kThreads * N);
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) tops[p] = take(held[p]);
+    for (int p = 0; p < kPieces; ++p) tops[p] = (unsigned)(p * kThreads * N) < length ? take(v[p]) : -INFINITY;
   } else {
     constexpr int kAhead = 4;
-    for (int64_t at = first; at < end; at += kAhead * kThreads * N) {
+    for (unsigned at = mine_at; at < length; at += kAhead * kThreads * N) {
       Vec<T, N> v[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) v[i] = get(at + (int64_t)i * kThreads * N, (T)-INFINITY);
+      for (int i = 0; i < kAhead; ++i) v[i] = get(at + i * kThreads * N);
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) take(v[i]);
     }
   }
+  if (wave == 0) {
+    if (x_outer > mine.m) mine.raise(x_outer);
+    mine.add(x_outer);
+  }
   if constexpr (ALT) {
-    float most = tops[0];
-#pragma unroll
-    for (int p = 1; p < kPieces; ++p) most = fmaxf(most, tops[p]);
-#pragma unroll
-    for (int p = 0; p < kPieces; ++p) {   // (what is looked at again is converted again: kept as 32-bit numbers it would take the registers of a wavefront)
-      Vec<unsigned, 4> words = __builtin_bit_cast(Vec<unsigned, 4>, held[p]);
-      asm volatile("" : "+v"(words.at[0]), "+v"(words.at[1]), "+v"(words.at[2]), "+v"(words.at[3]));
-      held[p] = __builtin_bit_cast(Held, words);
-    }
+    float most = mine.m;
     most = fmaxf(most, across<1>(most));
     most = fmaxf(most, across<2>(most));
     most = fmaxf(most, across<4>(most));
-    if ((lane & 7) == 0) group_tops[wave * 8 + (lane >> 3)] = most;
+    const int group = wave * 8 + (lane >> 3);   // (the last bits give way to the group's number, so that no two are equal)
+    if ((lane & 7) == 0) group_tops[group] = (in_order(most) & ~(kGroups - 1u)) | group;
     if (threadIdx.x == 0) collected = 0;
   }
   const Stats sums = wave_stats(mine);
   if (lane == 0) wave_sums[wave] = sums;
   __syncthreads();
   if constexpr (ALT) {
-    const float mine_of_groups = group_tops[lane & (kGroups - 1)];
+    const unsigned mine_of_groups = group_tops[lane & (kGroups - 1)];
     int larger = 0;
 #pragma unroll
     for (int g = 0; g < kGroups; g += 4) {
-      const Vec<float, 4> others = load_vec<float, 4>(group_tops + g);
+      const Vec<unsigned, 4> others = load_vec<unsigned, 4>(group_tops + g);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) larger += others.at[i] > mine_of_groups || (others.at[i] == mine_of_groups && g + i < (lane & (kGroups - 1)));
+      for (int i = 0; i < 4; ++i) larger += others.at[i] > mine_of_groups;
     }
     const unsigned long long at_bar = __ballot(larger == k - 1);
-    const float bar = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine_of_groups), __builtin_ctzll(at_bar)));
+    // (at or a little below the k-th largest, and not below the lowest number: with no piece above that, the largest is taken as that)
+    const float bar = out_of_order(__builtin_amdgcn_readlane(mine_of_groups, __builtin_ctzll(at_bar)) & ~(kGroups - 1u));
+    unsigned again = 0;   // pieces of which a lane has one
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) {
-      if (tops[p] >= bar) {
-        const int64_t id = first + (int64_t)p * kThreads * N;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float x = logit(held[p].at[i]);
-          if (x >= bar && x > -INFINITY) {   // (what is outside the part is held as minus infinity)
-            const int place = atomicAdd(&collected, 1);   // (in any order: places among them are found by value)
-            if (place < kRoom) candidates[place] = ranked(x, (unsigned)(id + i));
-          }
-        }
+    for (int p = 0; p < kPieces; ++p) again |= (unsigned)(__any(tops[p] >= bar) != 0) << p;
+    auto collect = [&](float x, int64_t id) {
+      if (x >= bar) {   // (what is masked or outside the part is minus infinity)
+        const int place = atomicAdd(&collected, 1);   // (in any order: places among them are found by value)
+        if (place < kRoom) candidates[place] = ranked(x + 0.f, (unsigned)id);
       }
+    };
+    if (wave == 0) collect(x_outer, outer);
+    for (; again; again &= again - 1) {
+      const unsigned at = mine_at + __builtin_ctz(again) * kThreads * N;
+      const Vec<T, N> v = get(at);
+#pragma unroll
+      for (int i = 0; i < N; ++i) collect((float)v.at[i], inner + at + i);
     }
     __syncthreads();
   }
   const bool whole = part_out.parts == 1;
   const int64_t at = row * part_out.parts + part;
   if (wave == 0) {
-    Stats all = wave_sums[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) all.join(wave_sums[w]);
+    const Stats all = put_together(wave_sums, lane);
     if (lane == 0) {
       if (whole) row_out.put(row, all, given, is_given);
       else part_out.stats[at] = all;
@@ -324,7 +331,14 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(RowOut<T> row_o
     bool is_given;
     const float given = row_out.given(row, &is_given);
     Stats mine = nothing();
-    for (int p = lane; p < part_out.parts; p += 64) mine.join(part_out.stats[row * part_out.parts + p]);
+    for (int p = lane; p < part_out.parts; p += 64) {
+      Stats other = part_out.stats[row * part_out.parts + p];
+      const float most = fmaxf(mine.m, other.m);
+      mine.raise(most);
+      other.raise(most);
+      mine.s += other.s;
+      mine.w += other.w;
+    }
     mine = wave_stats(mine);
     if (lane == 0) {
       all = mine;
