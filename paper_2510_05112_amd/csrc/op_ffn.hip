@@ -191,19 +191,23 @@ __device__ __forceinline__ void tile_of(unsigned id, int tiles_m, int tiles_n, i
 // hidden will be: the backward pass writes the three in the place of the two, whose memory then lasts until the weights' gradients.
 template <int N>
 struct Kept {
-  Vec<unsigned short, N> g, u;
-  Vec<unsigned char, 2 * N> last;
+  static_assert(N % 2 == 0, "two elements a word");
+  Vec<unsigned, N / 2> g, u, last;
 
   static __device__ __forceinline__ unsigned bits(float x) { return x == x ? __float_as_uint(x) + 0x80u : 0x7fc00000u; }
-  __device__ __forceinline__ void set(int e, float gate, float up) {
-    const unsigned bg = bits(gate), bu = bits(up);
-    g.at[e] = (unsigned short)(bg >> 16);
-    u.at[e] = (unsigned short)(bu >> 16);
-    last.at[2 * e] = (unsigned char)(bg >> 8);
-    last.at[2 * e + 1] = (unsigned char)(bu >> 8);
+  __device__ __forceinline__ void set(int pair, float gate0, float gate1, float up0, float up1) {
+    const unsigned g0 = bits(gate0), g1 = bits(gate1), u0 = bits(up0), u1 = bits(up1);
+    g.at[pair] = g0 >> 16 | (g1 & 0xffff0000u);
+    u.at[pair] = u0 >> 16 | (u1 & 0xffff0000u);
+    last.at[pair] = (g0 >> 8 & 0xff) | (u0 & 0xff00) | (g1 << 8 & 0xff0000) | (u1 << 16 & 0xff000000u);
   }
-  __device__ __forceinline__ float gate(int e) const { return __uint_as_float((unsigned)g.at[e] << 16 | (unsigned)last.at[2 * e] << 8); }
-  __device__ __forceinline__ float up(int e) const { return __uint_as_float((unsigned)u.at[e] << 16 | (unsigned)last.at[2 * e + 1] << 8); }
+  // (the bytes of an element from its two words, and 0 for the last one)
+  __device__ __forceinline__ float gate(int e) const {
+    return __uint_as_float(__builtin_amdgcn_perm(g.at[e / 2], last.at[e / 2], e % 2 ? 0x0706020c : 0x0504000c));
+  }
+  __device__ __forceinline__ float up(int e) const {
+    return __uint_as_float(__builtin_amdgcn_perm(u.at[e / 2], last.at[e / 2], e % 2 ? 0x0706030c : 0x0504010c));
+  }
 
   static __device__ __forceinline__ unsigned short* first_of(const Gemm& a, int64_t m, int64_t n) {
     return static_cast<unsigned short*>(a.kept) + m * 2 * a.n_half + n;
@@ -211,15 +215,16 @@ struct Kept {
   static __device__ __forceinline__ unsigned char* last_of(const Gemm& a, int64_t m, int64_t n) {
     return static_cast<unsigned char*>(a.kept) + (a.m.extent * 2 + m) * 2 * a.n_half + 2 * n;
   }
+  static __device__ __forceinline__ unsigned* words(void* p) { return static_cast<unsigned*>(p); }
   __device__ __forceinline__ void store(const Gemm& a, int64_t m, int64_t n) const {
-    store_vec<unsigned short, N>(first_of(a, m, n), g);
-    store_vec<unsigned short, N>(first_of(a, m, n) + a.n_half, u);
-    store_vec<unsigned char, 2 * N>(last_of(a, m, n), last);
+    store_vec<unsigned, N / 2>(words(first_of(a, m, n)), g);
+    store_vec<unsigned, N / 2>(words(first_of(a, m, n) + a.n_half), u);
+    store_vec<unsigned, N / 2>(words(last_of(a, m, n)), last);
   }
   __device__ __forceinline__ void load(const Gemm& a, int64_t m, int64_t n) {
-    g = load_vec<unsigned short, N>(first_of(a, m, n));
-    u = load_vec<unsigned short, N>(first_of(a, m, n) + a.n_half);
-    last = load_vec<unsigned char, 2 * N>(last_of(a, m, n));
+    g = load_vec<unsigned, N / 2>(words(first_of(a, m, n)));
+    u = load_vec<unsigned, N / 2>(words(first_of(a, m, n) + a.n_half));
+    last = load_vec<unsigned, N / 2>(words(last_of(a, m, n)));
   }
 };
 
@@ -231,23 +236,41 @@ __device__ __forceinline__ void put_gated(const Gemm& a, int64_t m, int64_t n, c
 #pragma unroll
   for (int e = 0; e < N; ++e) {
     h.at[e] = (T)(activate(a.act, gate.at[e]) * up.at[e]);
-    kept.set(e, gate.at[e], up.at[e]);
+    if (e % 2) kept.set(e / 2, gate.at[e - 1], gate.at[e], up.at[e - 1], up.at[e]);
   }
   store_vec<T, N>(static_cast<T*>(a.out) + m * a.out_stride + n, h);
   if (a.kept) kept.store(a, m, n);
 }
 
-// ... of 8 neighbouring columns of a row where there are no halves.
+// What is read of 8 neighbouring columns of a row's place before they are written, where there are no halves.
+template <int EPILOGUE, typename O>
+struct Before {
+  static constexpr bool kAny = std::is_same<O, float>::value;
+  Vec<O, 8> v;
+  __device__ __forceinline__ void load(const Gemm& a, int64_t m, int64_t n) {
+    if (!kAny || !a.accumulate) return;
+    const O* out = static_cast<const O*>(a.out) + m * a.out_stride + n;
+    const Vec<O, 4> low = load_vec<O, 4>(out), high = load_vec<O, 4>(out + 4);   // (rows begin at 16 bytes)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v.at[e] = low.at[e], v.at[e + 4] = high.at[e];
+  }
+};
+template <typename O>
+struct Before<kGatedGrad, O> {
+  static constexpr bool kAny = true;
+  Kept<8> kept;
+  __device__ __forceinline__ void load(const Gemm& a, int64_t m, int64_t n) { kept.load(a, m, n); }
+};
+
+// What becomes of them.
 template <typename T, int EPILOGUE, typename O>
-__device__ __forceinline__ void put_columns(const Gemm& a, int64_t m, int64_t n, const Vec<float, 8>& x) {
+__device__ __forceinline__ void put_columns(const Gemm& a, int64_t m, int64_t n, const Vec<float, 8>& x, const Before<EPILOGUE, O>& before) {
   if constexpr (EPILOGUE == kGatedGrad) {
-    Kept<8> kept;
-    kept.load(a, m, n);
-    asm volatile("" : : : "memory");   // (what is written below is of another type, in the same place)
+    asm volatile("" : : : "memory");   // (what is written below is of another type, in the place that `before` was read from)
     Vec<T, 8> dg, du, h;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float gate = kept.gate(e), up = kept.up(e), act = activate(a.act, gate);
+      const float gate = before.kept.gate(e), up = before.kept.up(e), act = activate(a.act, gate);
       dg.at[e] = (T)(x.at[e] * up * slope(a.act, gate));
       du.at[e] = (T)(x.at[e] * act);
       h.at[e] = (T)(act * up);
@@ -258,15 +281,10 @@ __device__ __forceinline__ void put_columns(const Gemm& a, int64_t m, int64_t n,
     store_vec<T, 8>(reinterpret_cast<T*>(Kept<8>::last_of(a, m, n)), h);
   } else {
     O* out = static_cast<O*>(a.out) + m * a.out_stride + n;
-    Vec<O, 8> v = {};
-    if (std::is_same<O, float>::value && a.accumulate) {
-      const Vec<O, 4> low = load_vec<O, 4>(out), high = load_vec<O, 4>(out + 4);
+    Vec<O, 8> v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v.at[e] = low.at[e], v.at[e + 4] = high.at[e];
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v.at[e] = (O)((float)v.at[e] + x.at[e]);
-    if constexpr (std::is_same<O, float>::value) {   // (rows begin at 16 bytes)
+    for (int e = 0; e < 8; ++e) v.at[e] = (O)(Before<EPILOGUE, O>::kAny && a.accumulate ? (float)before.v.at[e] + x.at[e] : x.at[e]);
+    if constexpr (std::is_same<O, float>::value) {
       store_vec<O, 4>(out, {v.at[0], v.at[1], v.at[2], v.at[3]});
       store_vec<O, 4>(out + 4, {v.at[4], v.at[5], v.at[6], v.at[7]});
     } else {
@@ -367,6 +385,18 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
   meet();   // (the loads of the tile behind the last one, zeros, among them)
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kPad;
   static_assert(kThreads / 64 * 32 * kPad * 4 <= 2 * kTile, "the rows fit");
+  constexpr int kColumns = (kHalves ? NF / 2 : NF) * 32, kLanes = kColumns / 8, kRows = 64 / kLanes;   // of the output; lanes of a row, rows at a time
+  const int64_t n = n0 + wave_n * kColumns + lane % kLanes * 8;
+  // What is read there is on its way 32 rows ahead.  (Read where it is needed, one wait after another: the gate's gradient of 8,192 x 10,752 x 4,096
+  // 799 us, and 778 so; weights' gradients added to what is there, 2,048 x 4,096 x 10,752, 685 and 648.)
+  using Ahead = Before<EPILOGUE, O>;
+  Ahead before[32 / kRows];
+  auto read_ahead = [&](int i, int p) {
+    const int64_t m = m0 + (wave_m * MF + i) * 32 + p * kRows + lane / kLanes;
+    if (Ahead::kAny && !kHalves && !shared && m < a.m.extent && n < a.n.extent) before[p].load(a, m, n);
+  };
+#pragma unroll
+  for (int p = 0; p < 32 / kRows; ++p) read_ahead(0, p);
 #pragma unroll
   for (int i = 0; i < MF; ++i) {
 #pragma unroll
@@ -377,8 +407,6 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
                             {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]});
     __builtin_amdgcn_wave_barrier();
     const int64_t rows = m0 + (wave_m * MF + i) * 32;
-    constexpr int kColumns = (kHalves ? NF / 2 : NF) * 32, kLanes = kColumns / 8, kRows = 64 / kLanes;   // of the output; lanes of a row, rows at a time
-    const int64_t n = n0 + wave_n * kColumns + lane % kLanes * 8;
 #pragma unroll
     for (int p = 0; p < 32 / kRows; ++p) {
       const int r = p * kRows + lane / kLanes;
@@ -403,7 +431,8 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
                      {u0.at[0], u0.at[1], u0.at[2], u0.at[3], u1.at[0], u1.at[1], u1.at[2], u1.at[3]});
       } else {
         if (m >= a.m.extent || n >= a.n.extent) continue;
-        put_columns<T, EPILOGUE, O>(a, m, n, {x0.at[0], x0.at[1], x0.at[2], x0.at[3], x1.at[0], x1.at[1], x1.at[2], x1.at[3]});
+        put_columns<T, EPILOGUE, O>(a, m, n, {x0.at[0], x0.at[1], x0.at[2], x0.at[3], x1.at[0], x1.at[1], x1.at[2], x1.at[3]}, before[p]);
+        if (i + 1 < MF) read_ahead(i + 1, p);
       }
     }
     __builtin_amdgcn_wave_barrier();
@@ -523,14 +552,19 @@ __global__ __launch_bounds__(256) void add_shares_kernel(Gemm a) {
     return sum;
   };
   if constexpr (EPILOGUE == kGated) put_gated<T, 8>(a, m, n, total(c), total(SIDE / 2 + c));
-  else put_columns<T, EPILOGUE, O>(a, m, n, total(c));
+  else {
+    Before<EPILOGUE, O> before;
+    before.load(a, m, n);
+    put_columns<T, EPILOGUE, O>(a, m, n, total(c), before);
+  }
 }
 
 // How a product is cut: into tiles of 256 x 256, one workgroup to a compute unit, or of 128 x 128, two of them; and the tiles
 // of the last round, where they leave compute units idle, into shares of k, whose sums another kernel adds up.  What decides is an estimate:
-// a step of 64 k takes 1.63 us and what becomes of a tile 5 (of the gate's gradient 30, which is 0.8 MB a tile); of the small tiles 1.1 us, 0.65 with one workgroup to a compute
-// unit, and 3; sums are written and read at 8 TB/s, in a launch more.  (Measured: 1,344 tiles of 128 steps, five rounds and a quarter, 1.25 ms whole and 1.13
-// with the last quarter in four shares; 80 small tiles of 216 steps 134 us whole and 30 in six.)
+// a step of 64 k takes 1.63 us and what becomes of a tile 5 (of the gate's gradient 30: it reads and writes 0.8 MB a tile); of the small tiles 1.1 us, 0.65 with one workgroup to a compute
+// unit, and 3; sums are written and read at 8 TB/s, in a launch more.  (Measured, whole and so: W of
+// 8,192 x 4,096 x 10,752, whose 1,344 tiles are five rounds and a quarter, 1.80 and 1.69 ms; d_x of 509 x 2,560 x 6,912, 80 small tiles of 216 steps, 134
+// and 45 us.)
 struct Split {
   bool large;
   int tiles_m, tiles_n, whole, parts;

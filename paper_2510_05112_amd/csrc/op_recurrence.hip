@@ -10,7 +10,7 @@
 //
 // The backward pass is the same walk from the end, of e[t-1] = a[t] (grad[t] + e[t]), where e is the gradient of the state from
 // what follows.  It needs h[t-1] to 32 bits: the forward pass leaves the state in front of every block
-// of 64 steps (at most 1/16 of what it reads), and the wavefronts work out the rest again from gate and value, which the backward pass reads anyway.
+// of 64 steps (1/64 of gate and value in 16 bits), and the wavefronts work out the rest again from gate and value, which the backward pass reads anyway.
 #include "ops_common.h"
 
 #include <algorithm>
