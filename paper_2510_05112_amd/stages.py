@@ -55,7 +55,7 @@ class Recurrence(Layer):
         return both[..., :width], both[..., width:]
 
     def forward(self, x):
-        both = x @ self.weights["w"].t()
+        both = (x.reshape(-1, x.shape[-1]) @ self.weights["w"].t()).view(*x.shape[:-1], -1)
         done = stage_ops.gated_recurrence(*self._halves(both), keep=True)
         return x + done["out"], dict(x=x, both=both, states=done["kept"])
 
@@ -63,7 +63,7 @@ class Recurrence(Layer):
         import torch
         back = stage_ops.gated_recurrence_grad(grad, *self._halves(kept["both"]), kept["states"])
         both = torch.cat([back["gate"], back["value"]], -1)
-        return grad + both @ self.weights["w"], dict(both=both)
+        return grad + (both.view(-1, both.shape[-1]) @ self.weights["w"]).view(grad.shape), dict(both=both)
 
     def weight_grad(self, kept, grad_kept):
         width = self.weights["w"].shape[1]
@@ -93,8 +93,8 @@ class FeedForward(Layer):
 
 
 class Head(Layer):
-    """The last layer of the last stage: logits and the log probabilities of given tokens.  The loss is minus the mean of those over the tokens that
-    are none of the paddings, less ``entropy_bonus`` times the mean entropy of those rows."""
+    """The last layer of the last stage: logits and the log probabilities of given tokens.  The loss is minus the mean of those over the tokens of
+    the vocabulary (others are padding), less ``entropy_bonus`` times the mean entropy of those rows."""
 
     def __init__(self, vocab, width, dtype, entropy_bonus=0.0, device="cuda", generator=None):
         super().__init__(w=_normal((vocab, width), width ** -0.5, dtype, device, generator))
@@ -104,7 +104,7 @@ class Head(Layer):
         rows, tokens = x.reshape(-1, x.shape[-1]), tokens.reshape(-1)
         logits = rows @ self.weights["w"].t()
         done = stage_ops.token_logprobs(logits, tokens)
-        share = (tokens >= 0).float()
+        share = ((tokens >= 0) & (tokens < logits.shape[1])).float()
         share /= share.sum().clamp(min=1)
         loss = -(share * (done["logprob"] + self.entropy_bonus * done["entropy"])).sum()
         return loss, dict(x=rows, shape=x.shape, logits=logits, tokens=tokens, share=share, lse=done["lse"], entropy=done["entropy"])

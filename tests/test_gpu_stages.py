@@ -209,3 +209,23 @@ def test_measured_costs_go_to_the_tuner():
     # (no schedule is shorter than its busiest device's work)
     assert best and best[0]["makespan"] >= 8 * int(dur[1:4].sum(0).max())
     handle.close()
+
+
+def test_head_takes_tokens_outside_the_vocabulary_for_padding():
+    head = st.Head(50, 16, torch.bfloat16)
+    x = torch.randn(2, 5, 16, device="cuda").bfloat16()
+    tokens = torch.randint(0, 50, (2, 5), device="cuda")
+    tokens[0, 1], tokens[1, 4] = -1, -1
+    other = tokens.clone()
+    other[other < 0] = 50
+    assert torch.equal(head.forward(x, tokens)[0], head.forward(x, other)[0])
+
+
+def test_recurrence_layer_of_a_view():
+    layer = st.Recurrence(16, torch.bfloat16)
+    x = torch.randn(7, 3, 16, device="cuda").bfloat16()
+    views, rows = x.transpose(0, 1), x.transpose(0, 1).contiguous()
+    (y1, kept1), (y2, kept2) = layer.forward(views), layer.forward(rows)
+    assert torch.equal(y1, y2)
+    g = torch.randn_like(rows)
+    assert torch.equal(layer.input_grad(g, kept1)[0], layer.input_grad(g, kept2)[0])
