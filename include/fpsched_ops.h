@@ -17,7 +17,7 @@
  * included; a call allocates nothing, keeps nothing, and only enqueues kernels on hip_stream (a
  * hipStream_t, NULL = default stream), so it can be captured into a graph and replayed.  Two calls
  * may share a workspace, or a tensor that one of them writes, only if they run one after the other.
- * Workspaces are 16-byte aligned.  A size of 0 rows is no error: nothing is read, and what is
+ * Workspaces are 16-byte aligned, tensors to their elements.  A size of 0 rows is no error: nothing is read, and what is
  * written of a gradient over no rows is zero.  Sums, states and softmax statistics are held in 32
  * bits; an output of a 16-bit type is rounded once, to nearest even.  Results are the same bits
  * from call to call (no atomic decides an order of additions).
@@ -48,7 +48,7 @@ int fpsched_op_embedding(int device_id, int type, const void *table, int64_t tab
  * written, with zeros where no token is; with accumulate (out_type FPSCHED_F32 only) the sums are added
  * to what out holds, and rows without a token are left as they are.  grad: [n_tokens][width] of `type`,
  * rows grad_stride apart; out: [n_rows][width] of `type` or FPSCHED_F32, rows out_stride apart.
- * n_tokens < 2^31, n_rows < 2^31. */
+ * n_tokens < 2^30, n_rows < 2^31. */
 size_t fpsched_op_embedding_grad_workspace_bytes(int64_t n_rows, int64_t width, int64_t n_tokens);
 int fpsched_op_embedding_grad(int device_id, int type, const void *grad, int64_t grad_stride, int64_t n_rows,
                               int64_t width, const void *tokens, int tokens64, int64_t n_tokens, float scale,

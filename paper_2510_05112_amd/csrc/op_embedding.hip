@@ -18,7 +18,7 @@ namespace fpsched {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int64_t kMaxWidth = 1 << 20;   // (what the grids have room for)
+constexpr int64_t kMaxWidth = 1 << 20, kMaxSummed = 1 << 30;   // (what the grids have room for: 64 lanes for 16 tokens of a gradient)
 
 // ---- lookup ----------------------------------------------------------------------------------------------------------
 
@@ -26,24 +26,25 @@ template <typename T, int N>
 __global__ __launch_bounds__(kThreads) void embedding_kernel(const T* table, int64_t table_stride, int64_t n_rows, int64_t width,
                                                             const void* tokens, int tokens64, int64_t n_tokens, float scale, T* out,
                                                             int64_t out_stride, int lanes_shift) {
-  const int64_t t = ((int64_t)blockIdx.x << (8 - lanes_shift)) + (threadIdx.x >> lanes_shift);
-  if (t >= n_tokens) return;
-  const int64_t token = token_at(tokens, tokens64, t);
-  const bool real = token >= 0 && token < n_rows;
-  const T* from = table + (real ? token * table_stride : 0);
-  T* to = out + t * out_stride;
-  const int lanes = 1 << lanes_shift;
-  for (int64_t c = (int64_t)(threadIdx.x & (lanes - 1)) * N; c < width; c += (int64_t)lanes * N) {
-    if (c + N <= width) {
-      Vec<T, N> v = {};
-      if (real) {
-        v = load_vec<T, N>(from + c);
+  const int64_t step = (int64_t)gridDim.x << (8 - lanes_shift);   // (more than one each where a grid has no room for all)
+  for (int64_t t = ((int64_t)blockIdx.x << (8 - lanes_shift)) + (threadIdx.x >> lanes_shift); t < n_tokens; t += step) {
+    const int64_t token = token_at(tokens, tokens64, t);
+    const bool real = token >= 0 && token < n_rows;
+    const T* from = table + (real ? token * table_stride : 0);
+    T* to = out + t * out_stride;
+    const int lanes = 1 << lanes_shift;
+    for (int64_t c = (int64_t)(threadIdx.x & (lanes - 1)) * N; c < width; c += (int64_t)lanes * N) {
+      if (c + N <= width) {
+        Vec<T, N> v = {};
+        if (real) {
+          v = load_vec<T, N>(from + c);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v.at[i] = (T)((float)v.at[i] * scale);
+          for (int i = 0; i < N; ++i) v.at[i] = (T)((float)v.at[i] * scale);
+        }
+        store_vec<T, N>(to + c, v);
+      } else {
+        for (int64_t i = c; i < width; ++i) to[i] = real ? (T)((float)from[i] * scale) : (T)0.f;
       }
-      store_vec<T, N>(to + c, v);
-    } else {
-      for (int64_t i = c; i < width; ++i) to[i] = real ? (T)((float)from[i] * scale) : (T)0.f;
     }
   }
 }
@@ -485,7 +486,8 @@ int fpsched_op_embedding(int device_id, int type, const void* table, int64_t tab
   if (table_stride < width || out_stride < width) return FPSCHED_EINVAL;
   if (device_id < 0) return FPSCHED_ENODEV;
   if (n_tokens == 0 || width == 0) return FPSCHED_OK;
-  if ((n_rows > 0 && !table) || !tokens || !out) return FPSCHED_EINVAL;
+  const size_t element = type == FPSCHED_F32 ? 4 : 2;
+  if ((n_rows > 0 && !table) || !tokens || !out || !aligned(table, element) || !aligned(out, element)) return FPSCHED_EINVAL;
   OpsDevice g(device_id);
   if (!g.ok) return FPSCHED_EHIP;
   return with_type(type, [&](auto zero) {
@@ -493,7 +495,7 @@ int fpsched_op_embedding(int device_id, int type, const void* table, int64_t tab
     auto go = [&](auto n) {
       constexpr int N = decltype(n)::value;
       const int shift = row_lanes_shift(ceil_div(width, N));
-      embedding_kernel<T, N><<<dim3((unsigned)ceil_div(n_tokens, kThreads >> shift)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
+      embedding_kernel<T, N><<<dim3((unsigned)std::min(kMostGroups, ceil_div(n_tokens, kThreads >> shift))), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
           static_cast<const T*>(table), table_stride, n_rows, width, tokens, tokens64, n_tokens, scale, static_cast<T*>(out), out_stride, shift);
       return launched();
     };
@@ -503,7 +505,7 @@ int fpsched_op_embedding(int device_id, int type, const void* table, int64_t tab
 }
 
 size_t fpsched_op_embedding_grad_workspace_bytes(int64_t n_rows, int64_t width, int64_t n_tokens) {
-  if (n_rows < 0 || width < 0 || width > kMaxWidth || n_tokens < 0 || n_rows > 0x7ffffffell || n_tokens > 0x7fffffffll) return 0;
+  if (n_rows < 0 || width < 0 || width > kMaxWidth || n_tokens < 0 || n_rows > 0x7ffffffell || n_tokens >= kMaxSummed) return 0;
   return grad_workspace(width, n_tokens).bytes;
 }
 
@@ -512,11 +514,12 @@ int fpsched_op_embedding_grad(int device_id, int type, const void* grad, int64_t
                               int64_t out_stride, int accumulate, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
   if (type < FPSCHED_BF16 || type > FPSCHED_F32 || (out_type != type && out_type != FPSCHED_F32)) return FPSCHED_EINVAL;
   if (accumulate && out_type != FPSCHED_F32) return FPSCHED_EINVAL;
-  if (n_rows < 0 || width < 0 || width > kMaxWidth || n_tokens < 0 || n_rows > 0x7ffffffell || n_tokens > 0x7fffffffll) return FPSCHED_EINVAL;
+  if (n_rows < 0 || width < 0 || width > kMaxWidth || n_tokens < 0 || n_rows > 0x7ffffffell || n_tokens >= kMaxSummed) return FPSCHED_EINVAL;
   if (grad_stride < width || out_stride < width) return FPSCHED_EINVAL;
   if (device_id < 0) return FPSCHED_ENODEV;
   if (n_rows == 0 || width == 0) return FPSCHED_OK;
   if (!out || (n_tokens > 0 && (!grad || !tokens)) || !d_workspace || !aligned(d_workspace, 16)) return FPSCHED_EINVAL;
+  if (!aligned(out, out_type == FPSCHED_F32 ? 4 : 2) || !aligned(grad, type == FPSCHED_F32 ? 4 : 2)) return FPSCHED_EINVAL;
   const GradWorkspace w = grad_workspace(width, n_tokens);
   if (workspace_bytes < w.bytes) return FPSCHED_ENOMEM;
   OpsDevice g(device_id);

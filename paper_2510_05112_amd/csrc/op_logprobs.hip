@@ -19,6 +19,8 @@
 
 #include <float.h>
 
+#include <algorithm>
+
 namespace fpsched {
 namespace {
 
@@ -141,6 +143,14 @@ struct RowOut {
   int32_t* ids;
   float* alternatives;
 
+  RowOut behind(int64_t rows) const {
+    RowOut r = *this;
+    r.logits += rows * stride;
+    r.tokens = static_cast<const char*>(tokens) + rows * (tokens64 ? 8 : 4);
+    r.logprob += rows, r.entropy += rows, r.lse += 2 * rows;
+    if (k) r.ids += rows * k, r.alternatives += rows * k;
+    return r;
+  }
   // the given token's logit; 0 and false if it has none
   __device__ __forceinline__ float given(int64_t row, bool* is) const {
     const int64_t token = token_at(tokens, tokens64, row);
@@ -368,8 +378,8 @@ template <typename T, int N>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(const T* logits, int64_t stride, int64_t vocab, const void* tokens,
                                                                 int tokens64, const float* lse, const float* entropy,
                                                                 const float* grad_logprob, const float* grad_entropy, T* out,
-                                                                int64_t out_stride, int pieces) {
-  const int64_t row = blockIdx.x / pieces;
+                                                                int64_t out_stride, int pieces, int64_t first_row) {
+  const int64_t row = first_row + blockIdx.x / pieces;
   const int64_t token = token_at(tokens, tokens64, row);
   const bool given = token >= 0 && token < vocab;
   const float m = lse[2 * row], ln = lse[2 * row + 1];
@@ -454,14 +464,19 @@ int fpsched_op_logprobs(int device_id, int type, int64_t n_rows, int64_t vocab, 
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   return with_type(type, [&](auto zero) {
     using T = decltype(zero);
-    const RowOut<T> row{static_cast<const T*>(logits), logits_stride, vocab, tokens, tokens64, n_alternatives, logprob, entropy, lse, ids, alternatives};
+    RowOut<T> row{static_cast<const T*>(logits), logits_stride, vocab, tokens, tokens64, n_alternatives, logprob, entropy, lse, ids, alternatives};
     PartOut part{static_cast<Stats*>(d_workspace), nullptr, p.parts};
     if (p.parts > 1)
       part.best = reinterpret_cast<unsigned long long*>(static_cast<char*>(d_workspace) + round_up((size_t)n_rows * p.parts * sizeof(Stats), 16));
-    const dim3 grid((unsigned)(n_rows * p.parts));
-    if (n_alternatives > 0) logprobs_kernel<T, true><<<grid, dim3(kThreads), 0, stream>>>(row, part, p.length);
-    else logprobs_kernel<T, false><<<grid, dim3(kThreads), 0, stream>>>(row, part, p.length);
-    if (p.parts > 1) logprobs_join_kernel<T><<<dim3((unsigned)n_rows), dim3(kThreads), 0, stream>>>(row, part);
+    const int64_t most = kMostGroups / p.parts;   // rows of a launch
+    for (int64_t at = 0; at < n_rows; at += most) {
+      const int64_t n = std::min(most, n_rows - at);
+      const dim3 grid((unsigned)(n * p.parts));
+      if (n_alternatives > 0) logprobs_kernel<T, true><<<grid, dim3(kThreads), 0, stream>>>(row, part, p.length);
+      else logprobs_kernel<T, false><<<grid, dim3(kThreads), 0, stream>>>(row, part, p.length);
+      if (p.parts > 1) logprobs_join_kernel<T><<<dim3((unsigned)n), dim3(kThreads), 0, stream>>>(row, part);
+      row = row.behind(n);
+    }
     return launched();
   });
 }
@@ -482,10 +497,11 @@ int fpsched_op_logprobs_grad(int device_id, int type, int64_t n_rows, int64_t vo
     auto go = [&](auto n) {
       constexpr int N = decltype(n)::value;
       const int64_t pieces = ceil_div(vocab, 4 * kThreads * N);
-      if (n_rows * pieces > 0x7fffffffll) return (int)FPSCHED_EINVAL;
-      logprobs_grad_kernel<T, N><<<dim3((unsigned)(n_rows * pieces)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
-          static_cast<const T*>(logits), logits_stride, vocab, tokens, tokens64, lse, entropy, grad_logprob, grad_entropy, static_cast<T*>(out),
-          out_stride, (int)pieces);
+      const int64_t most = kMostGroups / pieces;   // rows of a launch
+      for (int64_t at = 0; at < n_rows; at += most)
+        logprobs_grad_kernel<T, N><<<dim3((unsigned)(std::min(most, n_rows - at) * pieces)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
+            static_cast<const T*>(logits), logits_stride, vocab, tokens, tokens64, lse, entropy, grad_logprob, grad_entropy, static_cast<T*>(out),
+            out_stride, (int)pieces, at);
       return launched();
     };
     if (wide_rows(logits, logits_stride, sizeof(T)) && wide_rows(out, out_stride, sizeof(T))) return go(std::integral_constant<int, kWide<T>>());

@@ -466,6 +466,8 @@ int fpsched_op_recurrence(int device_id, int type, int64_t n_batch, int64_t n_st
   if (device_id < 0) return FPSCHED_ENODEV;
   if (n_batch == 0 || width == 0) return FPSCHED_OK;
   if (!final_state || (n_steps > 0 && (!gate || !value || !out))) return FPSCHED_EINVAL;
+  for (const void* p : {gate, value, static_cast<const void*>(out)})
+    if (!aligned(p, type == FPSCHED_F32 ? 4 : 2)) return FPSCHED_EINVAL;
   const Cut s = cut(n_batch, n_steps, width);
   if (s.segments > 1) {
     if (!d_workspace || !aligned(d_workspace, 16)) return FPSCHED_EINVAL;
@@ -510,6 +512,8 @@ int fpsched_op_recurrence_grad(int device_id, int type, int64_t n_batch, int64_t
   if (device_id < 0) return FPSCHED_ENODEV;
   if (n_batch == 0 || width == 0) return FPSCHED_OK;
   if (n_steps > 0 && (!grad || !gate || !value || !kept || !d_gate || !d_value)) return FPSCHED_EINVAL;
+  for (const void* p : {grad, gate, value, static_cast<const void*>(d_gate), static_cast<const void*>(d_value)})
+    if (!aligned(p, type == FPSCHED_F32 ? 4 : 2)) return FPSCHED_EINVAL;
   const Cut s = cut(n_batch, n_steps, width);
   if (s.segments > 1) {
     if (!d_workspace || !aligned(d_workspace, 16)) return FPSCHED_EINVAL;

@@ -129,3 +129,15 @@ def test_lookup_and_gradient_of_a_table_of_more_than_4_gib():
     ids, at = torch.unique(tokens, return_inverse=True)
     oracle.assert_near(back[ids.cuda()], *oracle.embedding_grad(grad.cpu(), at, len(ids), 1.0, torch.bfloat16))
     assert int((back != 0).any(1).sum()) == 4
+
+
+def test_lookup_of_more_rows_than_a_grid_has_workgroups():
+    # (a workgroup moves a row of 256 that is not aligned, and a grid has 2^24 - 1 of them)
+    n, width = (1 << 24) + 83, 256
+    table = torch.randn(1000, width + 1, device="cuda").bfloat16()[:, :width]
+    tokens = torch.arange(n, device="cuda", dtype=torch.int32) % 1003 - 1
+    got = ops.embedding(table, tokens)
+    for first in (0, (1 << 24) - 100, n - 100):
+        at = tokens[first:first + 100].long()
+        want = torch.where(((at >= 0) & (at < 1000))[:, None], table[at.clamp(0, 999)], 0)
+        assert torch.equal(got[first:first + 100], want), first

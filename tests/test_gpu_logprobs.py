@@ -155,3 +155,22 @@ def test_more_than_2_to_the_32_logits():
     ops.token_logprobs_grad(logits, tokens, done["lse"], done["entropy"], torch.ones(n, device="cuda"), out=logits)
     p = math.exp(float(want[0]))
     assert abs(float(logits[n - 1, vocab - 1]) - (1 - p)) <= 2 ** -8 * (1 - p) + 1e-6
+
+
+@pytest.mark.parametrize("vocab,k", [(2, 0), (3, 2)])
+def test_more_rows_than_a_grid_has_workgroups(vocab, k):
+    # (a workgroup looks at a row, and a grid has 2^24 - 1 of them)
+    n = (1 << 24) + 83
+    rows = torch.randn(1000, vocab, device="cuda").bfloat16()
+    logits = rows.repeat(n // 1000 + 1, 1)[:n]
+    tokens = torch.full((n,), vocab - 1, device="cuda", dtype=torch.int32)
+    gl = torch.ones(n, device="cuda")
+    want, want_tokens = ops.token_logprobs(rows, tokens[:1000], k), tokens[:1000]
+    want_grad = ops.token_logprobs_grad(rows, want_tokens, want["lse"], want["entropy"], gl[:1000])
+    done = ops.token_logprobs(logits, tokens, k)
+    got = ops.token_logprobs_grad(logits, tokens, done["lse"], done["entropy"], gl, out=logits)
+    for first in (0, (n - 100) // 1000 * 1000):
+        of = slice(first, min(first + 1000, n))
+        for name, t in done.items():
+            assert torch.equal(t[of], want[name][:of.stop - first]), (name, first)
+        assert torch.equal(got[of], want_grad[:of.stop - first]), first

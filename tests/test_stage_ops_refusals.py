@@ -167,3 +167,19 @@ def test_python_functions_check_their_tensors():
         ops.token_logprobs(zeros(1, 64).expand(4, 64), tokens)
     with pytest.raises(fp.FpschedError):
         ops.embedding_grad(x, tokens, 9, workspace=torch.zeros(64, dtype=torch.uint8, device="cuda"))
+
+
+def test_more_tokens_than_a_gradient_has_room_for(lib):
+    assert called(lib.fpsched_op_embedding_grad, EMBEDDING_GRAD, n=1 << 30) == EINVAL
+    assert lib.fpsched_op_embedding_grad_workspace_bytes(10, 64, 1 << 30) == 0
+    assert lib.fpsched_op_embedding_grad_workspace_bytes(10, 64, (1 << 30) - 1) > 0
+
+
+@pytest.mark.parametrize("name,defaults,changes", [
+    ("embedding", EMBEDDING, [dict(table=P + 1), dict(out=P + 1), dict(type=2, out=P + 2)]),
+    ("embedding_grad", EMBEDDING_GRAD, [dict(grad=P + 1), dict(out=P + 2)]),
+    ("recurrence", RECURRENCE, [dict(gate=P + 1), dict(value=P + 1), dict(out=P + 1), dict(type=2, out=P + 2)]),
+    ("recurrence_grad", RECURRENCE_GRAD, [dict(grad=P + 1), dict(gate=P + 1), dict(value=P + 1), dict(d_gate=P + 1), dict(d_value=P + 1)])])
+def test_tensors_that_are_not_aligned_to_their_elements(lib, name, defaults, changes):
+    for change in changes:
+        assert called(getattr(lib, "fpsched_op_" + name), dict(defaults, device=0), **change) == EINVAL, change
