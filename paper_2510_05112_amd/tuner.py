@@ -330,28 +330,30 @@ def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_back
     inputs = tokens
     with torch.cuda.device(device):
         saved = [{name: g.clone() for name, g in layer.grads.items()} for stage in stages for layer in stage.layers if hasattr(layer, "grads")]
-        for s, stage in enumerate(stages):
-            times = []
-            for _ in range(repeats + 1):   # (the first: memory is allocated, code is loaded)
-                at = [torch.cuda.Event(enable_timing=True) for _ in range(4)]
-                at[0].record()
-                out, kept = stage.forward(inputs, targets)
-                at[1].record()
-                grad = 1.0 if out.dim() == 0 else torch.ones_like(out)
-                held[s] = kept_bytes(kept)
-                at_b = torch.cuda.Event(enable_timing=True)
-                at_b.record()
-                _, grad_kept = stage.input_grad(grad, kept)
-                at[2].record()
-                stage.weight_grad(kept, grad_kept)
-                at[3].record()
-                at[3].synchronize()
-                times.append((at[0].elapsed_time(at[1]), at_b.elapsed_time(at[2]), at[2].elapsed_time(at[3])))
-            us[1:4, s] = 1e3 * np.median(np.asarray(times[1:]), axis=0)
-            inputs = out
-        for layer, grads in zip([x for stage in stages for x in stage.layers if hasattr(x, "grads")], saved):
-            for name, g in grads.items():
-                layer.grads[name].copy_(g)
+        try:
+            for s, stage in enumerate(stages):
+                times = []
+                for _ in range(repeats + 1):   # (the first: memory is allocated, code is loaded)
+                    at = [torch.cuda.Event(enable_timing=True) for _ in range(4)]
+                    at[0].record()
+                    out, kept = stage.forward(inputs, targets)
+                    at[1].record()
+                    grad = 1.0 if out.dim() == 0 else torch.ones_like(out)
+                    held[s] = kept_bytes(kept)
+                    at_b = torch.cuda.Event(enable_timing=True)
+                    at_b.record()
+                    _, grad_kept = stage.input_grad(grad, kept)
+                    at[2].record()
+                    stage.weight_grad(kept, grad_kept)
+                    at[3].record()
+                    at[3].synchronize()
+                    times.append((at[0].elapsed_time(at[1]), at_b.elapsed_time(at[2]), at[2].elapsed_time(at[3])))
+                us[1:4, s] = 1e3 * np.median(np.asarray(times[1:]), axis=0)
+                inputs = out
+        finally:
+            for layer, grads in zip([x for stage in stages for x in stage.layers if hasattr(x, "grads")], saved):
+                for name, g in grads.items():
+                    layer.grads[name].copy_(g)
     if not split_backward:
         us[2] += us[3]
         us[3] = 0
