@@ -2,9 +2,10 @@
 
 Thin ctypes binding over ``libfpsched.so`` (HIP, gfx950).  It only marshals
 arguments: every step of the hot path -- dependency propagation, per-candidate
-reductions, top-k -- runs in the library's kernels.  PyTorch provides device
-memory and the stream, nothing else.  There is no CPU fallback: if the library
-is missing or no GPU is present, the device calls raise.
+reductions, top-k -- runs in the library's kernels, and so does every operator of
+``stage_ops``.  PyTorch provides device memory and the stream, nothing else, but for
+the dense projections of the model stages in ``stages``.  There is no CPU fallback: if the
+library is missing or no GPU is present, the device calls raise.
 """
 from . import stage_ops
 from .binding import (FLAG_DEADLOCK, FLAG_INCOMPLETE, FLAG_OVER_CAP, FpschedError, Problem,

@@ -4,17 +4,20 @@
 //   log p[token] = (x[token] - m) - log s,   entropy = log s - w / s,
 // and two parts of a row are put together by multiplying s by e^(m1 - m) and adding s (m1 - m) to w.  A lane looks at 16
 // bytes of logits at a time and changes its m only where one of them is larger.  Rows are cut into parts where there are fewer rows than
-// the chip has room for; a second kernel puts the parts together.
+// the chip has room for; a second kernel puts the parts together.  Bound by memory for many rows (4,096 x 65,536 bf16: 105 us, 5.1 TB/s), for few by
+// ten instructions a logit and by what each part costs beside its logits (61 x 262,144: 14.8 us and 4.9 for the parts).
 //
-// Alternatives: the lanes keep their logits of the part in registers.  Of 32 groups of lanes each has a largest logit, and k logits at least are
-// not below the k-th of these; those that are not are collected in LDS (little more than k of them),
-// and each finds its place by counting the larger ones.  Equal logits come by ascending id: a candidate is
-// the logit's bits, in an order in which they compare as integers, with the id behind.  Where too many are equal to the bar (a row of one value) the k are found one by one.
+// Alternatives: of 32 groups of lanes each has a largest logit, and k logits at least are
+// not below the k-th of these, the bar; each lane knows the largest of each of its pieces, and the pieces with one that is not below the bar are
+// read once more (from cache: there are about as many as alternatives) and those logits collected in LDS.  Each finds its place by counting the larger
+// ones.  Equal logits come by ascending id: a candidate is the logit's bits, in an order in which they compare as integers, with the id behind.
+// Where too many are equal to the bar (a row of one value) the k are found one by one.  (Kept in registers instead, the pieces left room for five wavefronts
+// a SIMD, and twice the code: 18.5 against 14.8 us for 61 x 262,144 bf16, 43.8 against 35.3 for 509 x 100,003 f16, 164 against 93 for 1,000 x 128,000 f32.)
 //
 // Masked logits are minus infinity, and x - m = -infinity gives e = 0, but 0 times it is NaN: factors are held at -1000.  m begins at the
 // type's lowest number and not at minus infinity, so that a row of masks needs no branch: its s stays 0.
 //
-// Gradient: one pass, element by element, bound by memory.
+// Gradient: one pass, element by element, bound by memory (4,096 x 65,536 bf16: 180 us, 6.0 TB/s).
 #include "ops_common.h"
 
 #include <float.h>
@@ -26,7 +29,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMostAlternatives = 32;
-constexpr int kHeld = 64;                              // logits a lane keeps for the alternatives
+constexpr int kHeld = 64;                              // logits of a lane where alternatives are wanted (32: 149 against 131 us for 2,000 x 50,257 f16, k 32)
 constexpr int64_t kHeldPart = (int64_t)kThreads * kHeld;
 
 __device__ __forceinline__ float held_back(float x) { return fmaxf(x, -1000.f); }   // (of what is no number -1000, and its e^x none)
@@ -414,7 +417,7 @@ struct Parts {
   int parts;
 };
 
-// Parts of a row: with alternatives what a workgroup's registers hold, fewer logits where there are few rows (1,024 workgroups
+// Parts of a row: with alternatives kHeld logits a lane, fewer where there are few rows (1,024 workgroups
 // fill the chip), but 4,096 at least.
 Parts parts_of(int64_t n_rows, int64_t vocab, int k) {
   const int64_t wanted = std::max<int64_t>(1, ceil_div(1024, std::max<int64_t>(1, n_rows)));

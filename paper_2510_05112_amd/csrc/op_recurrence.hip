@@ -6,7 +6,10 @@
 // each wavefront then takes its steps from the state that those in front of it leave.
 //
 // Few sequences of few channels leave most of the chip idle that way; they are cut into segments, whose maps
-// a first kernel works out, and each segment's workgroup begins by composing those in front of it.
+// a first kernel works out, and each segment's workgroup begins by composing those in front of it.  That reads gate and value twice, and is what
+// bounds a few long sequences: 65,536 steps of 2,560 in 16 bits 156 us for the maps (4.3 TB/s) and 205 for the walk (4.9).  Without segments, 16
+// sequences of 1,024 steps of 4,096 take 210 us for both passes (5.1 TB/s).  (One reading, workgroups waiting for the states that others make known: 311 us
+// for the first, but 122 against 81 for 4 sequences of 1,021 steps of 4,096 both ways.)
 //
 // The backward pass is the same walk from the end, of e[t-1] = a[t] (grad[t] + e[t]), where e is the gradient of the state from
 // what follows.  It needs h[t-1] to 32 bits: the forward pass leaves the state in front of every block
