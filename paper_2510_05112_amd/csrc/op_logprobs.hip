@@ -11,8 +11,10 @@
 // not below the k-th of these, the bar; each lane knows the largest of each of its pieces, and the pieces with one that is not below the bar are
 // read once more (from cache: there are about as many as alternatives) and those logits collected in LDS.  Each finds its place by counting the larger
 // ones.  Equal logits come by ascending id: a candidate is the logit's bits, in an order in which they compare as integers, with the id behind.
-// Where too many are equal to the bar (a row of one value) the k are found one by one.  (Kept in registers instead, the pieces left room for five wavefronts
-// a SIMD, and twice the code: 18.5 against 14.8 us for 61 x 262,144 bf16, 43.8 against 35.3 for 509 x 100,003 f16, 164 against 93 for 1,000 x 128,000 f32.)
+// Where too many are not below the bar (a row of one value) the k-th largest is found digit by digit (509 x 100,003 equal f16 logits: 258 us, and
+// 514 where the k were found one by one).  The parts' candidates, which are in order, are put together by a bar of their own (1 x 4,500,000 f16, k 32: 31 us,
+// and 2,030 without).  (With the pieces kept in registers instead, there was room for five wavefronts a SIMD and twice the code: 18.5 against 14.8 us for
+// 61 x 262,144 bf16, 43.8 against 35.3 for 509 x 100,003 f16, 164 against 93 for 1,000 x 128,000 f32.)
 //
 // Masked logits are minus infinity, and x - m = -infinity gives e = 0, but 0 times it is NaN: factors are held at -1000.  m begins at the
 // type's lowest number and not at minus infinity, so that a row of masks needs no branch: its s stays 0.
@@ -112,7 +114,7 @@ __device__ __forceinline__ unsigned long long wave_most(unsigned long long a) {
   return a;
 }
 
-constexpr int kGroups = 8 * kWaves;   // of eight lanes
+constexpr int kGroups = 32;   // of the lanes of one number modulo 32: neighbouring logits are in different ones, and a part of 256 has some in each
 static_assert(kMostAlternatives <= kGroups, "as many groups of lanes as alternatives");
 constexpr int kRoom = 512;   // candidates in LDS
 
@@ -184,7 +186,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_ker
   constexpr int N = kWide<T>;
   __shared__ Stats wave_sums[kWaves];
   __shared__ unsigned long long candidates[ALT ? kRoom : 1];
-  __shared__ __align__(16) unsigned group_tops[kGroups];
+  __shared__ struct { unsigned digit, count, larger; } chosen;
+  __shared__ unsigned group_tops[ALT ? kWaves : 1][kGroups];
   __shared__ int collected;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = row_out.k;
   const int64_t row = blockIdx.x / part_out.parts, part = blockIdx.x % part_out.parts;
@@ -245,37 +248,32 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_ker
     mine.add(x_outer);
   }
   if constexpr (ALT) {
-    float most = mine.m;
-    most = fmaxf(most, across<1>(most));
-    most = fmaxf(most, across<2>(most));
-    most = fmaxf(most, across<4>(most));
-    const int group = wave * 8 + (lane >> 3);   // (the last bits give way to the group's number, so that no two are equal)
-    if ((lane & 7) == 0) group_tops[group] = (in_order(most) & ~(kGroups - 1u)) | group;
+    const float most = fmaxf(mine.m, across<32>(mine.m));   // (the last bits give way to the group's number, so that no two are equal)
+    if (lane < kGroups) group_tops[wave][lane] = (in_order(most) & ~(kGroups - 1u)) | lane;
     if (threadIdx.x == 0) collected = 0;
   }
   const Stats sums = wave_stats(mine);
   if (lane == 0) wave_sums[wave] = sums;
   __syncthreads();
   if constexpr (ALT) {
-    const unsigned mine_of_groups = group_tops[lane & (kGroups - 1)];
+    unsigned mine_of_groups = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) mine_of_groups = max(mine_of_groups, group_tops[w][lane & (kGroups - 1)]);
     int larger = 0;
 #pragma unroll
-    for (int g = 0; g < kGroups; g += 4) {
-      const Vec<unsigned, 4> others = load_vec<unsigned, 4>(group_tops + g);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) larger += others.at[i] > mine_of_groups;
-    }
+    for (int g = 0; g < kGroups; ++g) larger += (unsigned)__builtin_amdgcn_readlane(mine_of_groups, g) > mine_of_groups;
     const unsigned long long at_bar = __ballot(larger == k - 1);
     // (at or a little below the k-th largest, and not below the lowest number: with no piece above that, the largest is taken as that)
     const float bar = out_of_order(__builtin_amdgcn_readlane(mine_of_groups, __builtin_ctzll(at_bar)) & ~(kGroups - 1u));
     unsigned again = 0;   // pieces of which a lane has one
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) again |= (unsigned)(__any(tops[p] >= bar) != 0) << p;
+    auto add = [&](unsigned long long r) {
+      const int place = atomicAdd(&collected, 1);   // (in any order: places among them are found by value)
+      if (place < kRoom) candidates[place] = r;
+    };
     auto collect = [&](float x, int64_t id) {
-      if (x >= bar) {   // (what is masked or outside the part is minus infinity)
-        const int place = atomicAdd(&collected, 1);   // (in any order: places among them are found by value)
-        if (place < kRoom) candidates[place] = ranked(x + 0.f, (unsigned)id);
-      }
+      if (x >= bar) add(ranked(x + 0.f, (unsigned)id));   // (what is masked or outside the part is minus infinity)
     };
     if (wave == 0) collect(x_outer, outer);
     for (; again; again &= again - 1) {
@@ -285,38 +283,74 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_ker
       for (int i = 0; i < N; ++i) collect((float)v.at[i], inner + at + i);
     }
     __syncthreads();
+    if (collected > kRoom) {
+      // Too many (more than kRoom equal logits, say): the k-th largest candidate's digits of eight bits are counted out, from the first on in which the
+      // largest and the smallest that there can be differ, until few enough are not below what is known of it.
+      auto all_of_part = [&](auto f) {
+        auto one = [&](float x, int64_t id) {
+          if (x > -INFINITY) f(ranked(x + 0.f, (unsigned)id));
+        };
+        if (wave == 0) one(x_outer, outer);
+        for (unsigned at = mine_at; at < length; at += kThreads * N) {
+          const Vec<T, N> v = get(at);
+#pragma unroll
+          for (int i = 0; i < N; ++i) one((float)v.at[i], inner + at + i);
+        }
+      };
+      unsigned* counts = reinterpret_cast<unsigned*>(candidates);
+      static_assert(kThreads == 256 && (!ALT || sizeof(candidates) >= kThreads * 4), "a digit a lane");
+      const unsigned long long largest = ranked(put_together(wave_sums, lane).m + 0.f, (unsigned)begin), smallest = ranked(bar, (unsigned)(end - 1));
+      int shift = (63 - __builtin_clzll((largest ^ smallest) | 1)) & ~7;
+      unsigned long long known = shift == 56 ? 0 : largest >> (shift + 8) << (shift + 8);
+      unsigned wanted = k;   // of those that begin with what is known
+      for (; shift >= 0; shift -= 8) {
+        __syncthreads();
+        counts[threadIdx.x] = 0;
+        __syncthreads();
+        all_of_part([&](unsigned long long r) {
+          if (shift == 56 || (r ^ known) >> (shift + 8) == 0) {
+            const unsigned digit = (unsigned)(r >> shift) & 255, of_first = __builtin_amdgcn_readfirstlane(digit);
+            const unsigned long long here = __ballot(1);
+            if (__ballot(digit == of_first) == here) {   // (as digits of equal logits are: one addition for all lanes)
+              if (__builtin_ctzll(here) == lane) atomicAdd(&counts[digit], (unsigned)__popcll(here));
+            } else {
+              atomicAdd(&counts[digit], 1u);
+            }
+          }
+        });
+        __syncthreads();
+        unsigned larger = 0;
+        for (int d = kThreads - 1; d >= 0; --d) larger += d > (int)threadIdx.x ? counts[d] : 0u;
+        const unsigned count = counts[threadIdx.x];
+        if (larger < wanted && larger + count >= wanted) chosen = {threadIdx.x, count, larger};
+        __syncthreads();
+        known |= (unsigned long long)chosen.digit << shift;
+        wanted -= chosen.larger;
+        if (k - wanted + chosen.count <= kRoom) break;
+      }
+      if (threadIdx.x == 0) collected = 0;
+      __syncthreads();
+      all_of_part([&](unsigned long long r) {
+        if (r >= known) add(r);
+      });
+      __syncthreads();
+    }
   }
   const bool whole = part_out.parts == 1;
   const int64_t at = row * part_out.parts + part;
-  if (wave == 0) {
-    const Stats all = put_together(wave_sums, lane);
-    if (lane == 0) {
-      if (whole) row_out.put(row, all, given, is_given);
-      else part_out.stats[at] = all;
-    }
-    if constexpr (ALT) {
-      const int n = collected;
-      auto put = [&](int i, unsigned long long r) {
-        if (whole) row_out.put_alternative(row, i, r, all);
-        else part_out.best[at * k + i] = r;
-      };
-      if (n <= kRoom) {
-        for (int first = 0; first < n; first += 64) by_rank(candidates, n, k, first + lane, put);
-        if (lane >= n && lane < k) put(lane, 0);
-      } else {
-        unsigned long long below = ~0ull;
-        for (int i = 0; i < k; ++i) {
-          unsigned long long best = 0;
-          for (int64_t id = begin + lane; id < end; id += 64) {
-            const float x = logit(logits[id]);
-            const unsigned long long r = ranked(x, (unsigned)id);
-            if (x > -INFINITY && r < below && r > best) best = r;
-          }
-          below = wave_most(best);
-          if (lane == 0) put(i, below);
-        }
-      }
-    }
+  const Stats all = whole || wave == 0 ? put_together(wave_sums, lane) : nothing();
+  if (threadIdx.x == 0) {
+    if (whole) row_out.put(row, all, given, is_given);
+    else part_out.stats[at] = all;
+  }
+  if constexpr (ALT) {
+    const int n = collected;
+    auto put = [&](int i, unsigned long long r) {
+      if (whole) row_out.put_alternative(row, i, r, all);
+      else part_out.best[at * k + i] = r;
+    };
+    for (int first = wave * 64; first < n; first += kThreads) by_rank(candidates, n, k, first + lane, put);
+    if ((int)threadIdx.x >= n && (int)threadIdx.x < k) put(threadIdx.x, 0);
   }
 }
 
@@ -325,6 +359,7 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(RowOut<T> row_out, PartOut part_out) {
   constexpr int kRoomOfParts = 1024;
   __shared__ unsigned long long candidates[kRoomOfParts];
+  __shared__ unsigned long long tops[kThreads], bar;
   __shared__ Stats all;
   __shared__ int collected;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = row_out.k;
@@ -333,11 +368,35 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(RowOut<T> row_o
   const unsigned long long* best = part_out.best + row * n;
   if (threadIdx.x == 0) collected = 0;
   __syncthreads();
-  if (n <= kRoomOfParts) {
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      const unsigned long long r = best[i];
-      candidates[i] = r;
-      if (r) atomicAdd(&collected, 1);
+  auto add = [&](unsigned long long r) {
+    if (r == 0) return;
+    const int place = atomicAdd(&collected, 1);
+    if (place < kRoomOfParts) candidates[place] = r;
+  };
+  if (n <= kThreads || part_out.parts < k) {   // (fewer parts than alternatives have fewer candidates than kMostAlternatives^2)
+    for (int i = threadIdx.x; i < n; i += kThreads) add(best[i]);
+  } else {
+    // The parts' candidates are in order, so a part whose first one is below the bar has none; the bar is the k-th of the largest ones of the lanes' parts.
+    // Up to kThreads parts, k of them at most are not below it.
+    unsigned long long most = 0;
+    for (int p = threadIdx.x; p < part_out.parts; p += kThreads) {
+      const unsigned long long r = best[(int64_t)p * k];
+      most = r > most ? r : most;
+    }
+    tops[threadIdx.x] = most;
+    if (threadIdx.x == 0) bar = 1;
+    __syncthreads();
+    int larger = 0;
+#pragma unroll 16
+    for (int i = 0; i < kThreads; ++i) larger += tops[i] > most;
+    if (most && larger == k - 1) bar = most;   // (fewer lanes that have one: all candidates, fewer than kMostAlternatives^2 up to kThreads parts)
+    __syncthreads();
+    for (int p = threadIdx.x; p < part_out.parts; p += kThreads) {
+      for (int i = 0; i < k; ++i) {
+        const unsigned long long r = best[(int64_t)p * k + i];
+        if (r < bar) break;
+        add(r);
+      }
     }
   }
   if (wave == 0) {
@@ -359,10 +418,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(RowOut<T> row_o
     }
   }
   __syncthreads();
-  if (n <= kRoomOfParts) {
-    for (int first = wave * 64; first < n; first += kThreads)
-      by_rank(candidates, n, k, first + lane, [&](int i, unsigned long long r) { row_out.put_alternative(row, i, r, all); });
-    if ((int)threadIdx.x >= collected && (int)threadIdx.x < k) row_out.put_alternative(row, threadIdx.x, 0, all);
+  if (collected <= kRoomOfParts) {
+    const int found = collected;
+    for (int first = wave * 64; first < found; first += kThreads)
+      by_rank(candidates, found, k, first + lane, [&](int i, unsigned long long r) { row_out.put_alternative(row, i, r, all); });
+    if ((int)threadIdx.x >= found && (int)threadIdx.x < k) row_out.put_alternative(row, threadIdx.x, 0, all);
   } else if (wave == 0) {
     unsigned long long below = ~0ull;
     for (int i = 0; i < k; ++i) {

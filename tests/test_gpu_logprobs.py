@@ -174,3 +174,26 @@ def test_more_rows_than_a_grid_has_workgroups(vocab, k):
         for name, t in done.items():
             assert torch.equal(t[of], want[name][:of.stop - first]), (name, first)
         assert torch.equal(got[of], want_grad[:of.stop - first]), first
+
+
+@pytest.mark.parametrize("vocab", [300, 700, 2003, 16384, 40001, 262144])
+def test_alternatives_of_logits_in_any_order(vocab):
+    # (ascending, descending, of one value, of one value but for a few, few values with the largest at the end, masked but for few)
+    at = torch.arange(vocab)
+    rows = torch.stack([at * (9.0 / vocab), 5 - at * (9.0 / vocab), torch.full((vocab,), -2.5), torch.where(at % 677 == 3, 1.0, 0.5), (at > vocab - 600).float() + (at > vocab - 5).float(),
+                        torch.where(at % 97 == 5, at * (1.0 / vocab), -math.inf), torch.where(at % 301 == 0, -math.inf, -3.0), torch.where(at < 10, at * 1.0, torch.finfo(torch.float32).min)])
+    tokens = torch.full((len(rows),), vocab - 1)
+    for dtype in TYPES:
+        for k in (1, 7, 32):
+            check(rows.clamp(min=torch.finfo(dtype).min).where(rows > -math.inf, rows).to(dtype), tokens, k, what=f"{dtype} {k}")
+
+
+def test_alternatives_of_many_parts():
+    # (one row in a thousand parts: the largest logits in any of them; the last row has them in parts of which a lane takes several)
+    vocab = 4_500_000
+    at = torch.arange(vocab)
+    block = at // 4416 % 256
+    rows = torch.stack([torch.randn(vocab), torch.zeros(vocab), at * 1e-6, at * -1e-6, torch.where(block < 31, 5.0, torch.where(block == 31, 1.0, 0.0))])
+    for row in rows:
+        for k in (1, 8, 32):
+            check(row[None], torch.tensor([vocab - 1]), k, what=str(k))
