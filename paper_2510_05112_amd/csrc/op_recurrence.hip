@@ -6,7 +6,8 @@
 // each wavefront then takes its steps from the state that those in front of it leave.
 //
 // Few sequences of few channels leave most of the chip idle that way; they are cut into segments, whose maps
-// a first kernel works out, and each segment's workgroup begins by composing those in front of it.  That reads gate and value twice, and is what
+// a first kernel works out, and each segment's workgroup begins by composing those in front of it, a share a wavefront (one after the other, the thousand
+// maps of 65,536 steps of 64 channels took 261 us with everything, and 66 so).  That reads gate and value twice, and is what
 // bounds a few long sequences: 65,536 steps of 2,560 in 16 bits 156 us for the maps (4.3 TB/s) and 205 for the walk (4.9).  Without segments, 16
 // sequences of 1,024 steps of 4,096 take 210 us for both passes (5.1 TB/s).  (One reading, workgroups waiting for the states that others make known: 311 us
 // for the first, but 122 against 81 for 4 sequences of 1,021 steps of 4,096 both ways.)
@@ -135,15 +136,47 @@ __global__ __launch_bounds__(kWaves * 64) void segment_maps_kernel(RecurrenceArg
   }
 }
 
-// A lane's channels of the walk's state in front of its turn-th segment.
-template <typename T, int N>
-__device__ __forceinline__ void begin_walk(const RecurrenceArgs<T>& args, int64_t b, int turn, int segments, unsigned c, float (&h)[N]) {
+// A lane's channels of the walk's state in front of its turn-th segment.  Each wavefront composes a share of the maps in front, in order; the shares go
+// round through LDS (`maps`: a half of it that the walk's first block does not use).
+template <typename T, int N, int WAVES>
+__device__ __forceinline__ void begin_walk(const RecurrenceArgs<T>& args, int64_t b, int turn, int segments, unsigned c, int lane, int wave,
+                                           Vec<float, 2 * N> (&maps)[WAVES][64], float (&h)[N]) {
 #pragma unroll
   for (int k = 0; k < N; ++k) h[k] = args.state ? args.state[b * args.width + c + k] : 0.f;
-  const float* m = args.segment_maps + b * segments * 2 * args.width + c;
-  for (int s = 0; s < turn; ++s, m += 2 * args.width) {
+  if (turn == 0) return;
+  const int share = (turn + WAVES - 1) / WAVES, first = min(wave * share, turn), last = min(first + share, turn);
+  const float* m = args.segment_maps + (b * segments + first) * 2 * args.width + c;
+  Vec<float, 2 * N> mine;
 #pragma unroll
-    for (int k = 0; k < N; ++k) h[k] = m[k] * h[k] + m[args.width + k];
+  for (int k = 0; k < N; ++k) mine.at[k] = 1.f, mine.at[N + k] = 0.f;
+  constexpr int kAhead = 8;
+  for (int s = first; s < last; s += kAhead) {
+    float A[kAhead][N], S[kAhead][N];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const float* at = m + (int64_t)min(i, last - 1 - s) * 2 * args.width;
+#pragma unroll
+      for (int k = 0; k < N; ++k) A[i][k] = at[k], S[i][k] = at[args.width + k];
+    }
+    m += (int64_t)kAhead * 2 * args.width;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (s + i < last) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          mine.at[N + k] = A[i][k] * mine.at[N + k] + S[i][k];
+          mine.at[k] *= A[i][k];
+        }
+      }
+    }
+  }
+  maps[wave][lane] = mine;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    const Vec<float, 2 * N> o = maps[w][lane];
+#pragma unroll
+    for (int k = 0; k < N; ++k) h[k] = o.at[k] * h[k] + o.at[N + k];
   }
 }
 
@@ -160,8 +193,8 @@ __global__ __launch_bounds__(kWaves * 64, 4) void recurrence_kernel(RecurrenceAr
   const T *gate = args.gate + b * args.s_gate.batch, *value = args.value + b * args.s_value.batch;
   T* out = args.out + b * args.s_out.batch;
   float h[N];   // the state in front of the block
-  begin_walk<T, N>(args, b, segment, segments, c, h);
   const int first_block = segment * args.segment_blocks, last_block = min(first_block + args.segment_blocks, args.blocks);
+  begin_walk<T, N, kWaves>(args, b, segment, segments, c, lane, wave, maps[(first_block + 1) & 1], h);
   for (int block = first_block; block < last_block; ++block) {
     const int64_t first = (int64_t)block * kBlock + wave * kSteps;
     float a[kSteps][N], s[kSteps][N];
@@ -297,8 +330,8 @@ __global__ __launch_bounds__(kGradWaves * 64) void recurrence_grad_kernel(Recurr
   const T *gate = args.gate + b * args.s_gate.batch, *value = args.value + b * args.s_value.batch, *grad = args.grad + b * args.s_grad.batch;
   T *d_gate = args.d_gate + b * args.s_d_gate.batch, *d_value = args.d_value + b * args.s_d_value.batch;
   float e[N];   // the gradient of the state behind the block
-  begin_walk<T, N>(args, b, segments - 1 - segment, segments, c, e);
   const int first_block = segment * args.segment_blocks, last_block = min(first_block + args.segment_blocks, args.blocks);
+  begin_walk<T, N, kGradWaves>(args, b, segments - 1 - segment, segments, c, lane, wave, maps[last_block & 1], e);
   for (int block = last_block - 1; block >= first_block; --block) {
     const int64_t first = (int64_t)block * kBlock + wave * kGradSteps;
     Vec<T, N> g[kGradSteps], v[kGradSteps], d[kGradSteps];

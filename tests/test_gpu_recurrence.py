@@ -1,4 +1,5 @@
 """The gated linear recurrence and its gradients against the plain forms in 64 bits."""
+import numpy as np
 import pytest
 import torch
 
@@ -177,3 +178,24 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(got["out"], want["out"])
     back = [ops.gated_recurrence_grad(grad.cuda(), gate.cuda(), v, want["kept"]) for v in (store[None, :, 8:8 + width], value.cuda())]
     assert all(torch.equal(back[0][k], back[1][k]) for k in back[0])
+
+
+@pytest.mark.parametrize("width", [1, 6, 130])
+def test_many_segments(width):
+    # (one long sequence of few channels: a thousand segments, whose maps are composed by shares)
+    steps = 70001
+    g = torch.Generator().manual_seed(width)
+    gate, value, grad = (torch.randn(1, steps, width, generator=g) for _ in range(3))
+    a, v, d = torch.sigmoid(gate.double())[0].numpy(), value.double()[0].numpy(), grad.double()[0].numpy()
+    out, behind = np.empty_like(v), np.empty_like(v)
+    h = e = np.zeros(width)
+    for t in range(steps):
+        h = out[t] = a[t] * h + (1 - a[t]) * v[t]
+    for t in range(steps - 1, -1, -1):
+        behind[t] = d[t] + e
+        e = a[t] * behind[t]
+    done = ops.gated_recurrence(gate.cuda(), value.cuda(), keep=True)
+    # (a state forgets: a mean of values of 5 at most, its terms off by some 2^-21 of themselves; the gradient likewise)
+    assert np.abs(done["out"][0].cpu().double().numpy() - out).max() <= 1e-5
+    back = ops.gated_recurrence_grad(grad.cuda(), gate.cuda(), value.cuda(), done["kept"])
+    assert np.abs(back["value"][0].cpu().double().numpy() - behind * (1 - a)).max() <= 1e-5 * (1 + np.abs(behind).max())
