@@ -44,7 +44,8 @@ int fpsched_op_embedding(int device_id, int type, const void *table, int64_t tab
                          void *out, int64_t out_stride, void *hip_stream);
 
 /* The gradient of the table: out[v][:] = scale * sum of grad[t][:] over the t with tokens[t] == v, in
- * ascending t within blocks of 16 sorted occurrences and then over the blocks.  All n_rows rows are
+ * ascending t within blocks of 16 sorted occurrences and then over the blocks, in an order that the
+ * tokens alone decide.  All n_rows rows are
  * written, with zeros where no token is; with accumulate (out_type FPSCHED_F32 only) the sums are added
  * to what out holds, and rows without a token are left as they are.  grad: [n_tokens][width] of `type`,
  * rows grad_stride apart; out: [n_rows][width] of `type` or FPSCHED_F32, rows out_stride apart.

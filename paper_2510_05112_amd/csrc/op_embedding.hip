@@ -9,7 +9,8 @@
 // dE is the sum of a run of sorted occurrences.  Text repeats its few commonest tokens thousands of times: so that a
 // run's length bounds nothing, the sorted occurrences are cut into blocks of 16 without regard to runs, each summed by
 // workgroups of its own; a run inside one block is written where it belongs, one across blocks leaves its parts (32 bits) in the workspace, which
-// another kernel adds up.  Most rows of a large vocabulary have no token: all are filled with zeros by what the sort leaves of the chip.
+// another kernel adds up, of more than 16,384 tokens with sums over chunks of 64 blocks in between (131,072 tokens that are all the same, 1,024 wide: 767 us
+// by one wavefront a run, 193 so).  Most rows of a large vocabulary have no token: all are filled with zeros by what the sort leaves of the chip.
 // Floor: grad read once, dE written once.  Measured (bf16): 4,096 tokens into 65,536 x 4,096 sort and zeros 89 us (537 MB of zeros: 6.1 TB/s,
 // and a fill by itself reaches 6.9), sums 25, runs across blocks 8; 16,384 into 262,144 x 2,560 225 us, 46 and 11.
 #include "ops_common.h"
@@ -247,11 +248,12 @@ __global__ __launch_bounds__(1024) void sort_scan_kernel(unsigned* counts, int64
   __shared__ unsigned waves[16];
   unsigned before = 0;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t at = 0; at < n; at += 4096) {
-    const int64_t mine = at + threadIdx.x * 4;
-    unsigned c[4], sum = 0;
+  constexpr int kEach = 16;
+  for (int64_t at = 0; at < n; at += 1024 * kEach) {
+    const int64_t mine = at + threadIdx.x * kEach;
+    unsigned c[kEach], sum = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kEach; ++i) {
       c[i] = mine + i < n ? counts[mine + i] : 0u;
       sum += c[i];
     }
@@ -271,7 +273,7 @@ __global__ __launch_bounds__(1024) void sort_scan_kernel(unsigned* counts, int64
     }
     base += incl - sum;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kEach; ++i) {
       if (mine + i < n) counts[mine + i] = base;
       base += c[i];
     }
@@ -406,34 +408,23 @@ __global__ __launch_bounds__(64) void row_sums_kernel(const T* __restrict__ grad
   flush(!goes_on);
 }
 
-// The runs across blocks: the workgroups of the block that one begins in add up its parts.
-template <typename O, int N>
-__global__ __launch_bounds__(64) void join_runs_kernel(const Occurrence* __restrict__ sorted, const unsigned* __restrict__ n, int64_t width,
-                                                      const float* __restrict__ parts, int64_t part_stride, float scale,
-                                                      O* __restrict__ out, int64_t out_stride, int accumulate) {
-  const unsigned first = blockIdx.x * (unsigned)kBlock, all = *n, end = first + kBlock;
-  if (end >= all) return;
-  const unsigned token = sorted[end - 1].token;
-  if (sorted[end].token != token) return;
-  if (sorted[first].token == token && first > 0 && sorted[first - 1].token == token) return;   // (it begins further in front)
-  // the last block that has some of it (its tokens begin blocks up to there)
-  unsigned low = blockIdx.x + 1, high = (all - 1) / kBlock;
+// The last of blocks low .. high that begins with `token`, which low does (they are in order).
+__device__ __forceinline__ unsigned last_block_of(unsigned token, const Occurrence* sorted, unsigned low, unsigned high) {
   while (low < high) {
     const unsigned mid = (low + high + 1) >> 1;
-    if (sorted[mid * kBlock].token == token) low = mid; else high = mid - 1;
+    if (sorted[(int64_t)mid * kBlock].token == token) low = mid; else high = mid - 1;
   }
-  const int64_t c = ((int64_t)blockIdx.y * 64 + threadIdx.x) * N;
-  if (c >= width) return;
-  float sum[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) sum[i] = parts[(2 * (int64_t)blockIdx.x + 1) * part_stride + c + i];
-  const float* from = parts + 2 * (int64_t)(blockIdx.x + 1) * part_stride + c;
+  return low;
+}
+// The sum of n parts, part_stride apart, from `from` on.
+template <int N>
+__device__ __forceinline__ void sum_parts(const float* from, int64_t part_stride, unsigned n, float (&sum)[N]) {
   constexpr unsigned kAhead = 8;
-  unsigned b = blockIdx.x + 1;
-  for (; b + kAhead <= low + 1; b += kAhead) {
+  unsigned b = 0;
+  for (; b + kAhead <= n; b += kAhead) {
     float x[kAhead][N];
 #pragma unroll
-    for (unsigned j = 0; j < kAhead; ++j, from += 2 * part_stride)
+    for (unsigned j = 0; j < kAhead; ++j, from += part_stride)
 #pragma unroll
       for (int i = 0; i < N; ++i) x[j][i] = from[i];
 #pragma unroll
@@ -441,9 +432,70 @@ __global__ __launch_bounds__(64) void join_runs_kernel(const Occurrence* __restr
 #pragma unroll
       for (int i = 0; i < N; ++i) sum[i] += x[j][i];
   }
-  for (; b <= low; ++b, from += 2 * part_stride)
+  for (; b < n; ++b, from += part_stride)
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] += from[i];
+}
+
+// Long runs: what a run that comes into a chunk of kChunk blocks has in that chunk is summed into its first block's part.  blockIdx.x: chunk.
+constexpr unsigned kChunk = 64;
+template <int N>
+__global__ __launch_bounds__(64) void chunk_sums_kernel(const Occurrence* __restrict__ sorted, const unsigned* __restrict__ n, int64_t width, float* parts, int64_t part_stride) {
+  const unsigned first = blockIdx.x * kChunk, all = *n;
+  if (first == 0 || (int64_t)first * kBlock >= all) return;
+  const unsigned token = sorted[(int64_t)first * kBlock].token;
+  if (sorted[(int64_t)first * kBlock - 1].token != token) return;
+  const unsigned last = last_block_of(token, sorted, first, min((all - 1) / kBlock, first + kChunk - 1));
+  const int64_t c = ((int64_t)blockIdx.y * 64 + threadIdx.x) * N;
+  if (c >= width) return;
+  float sum[N] = {};
+  float* to = parts + 2 * (int64_t)first * part_stride + c;
+  sum_parts<N>(to, 2 * part_stride, last - first + 1, sum);
+#pragma unroll
+  for (int i = 0; i < N; ++i) to[i] = sum[i];
+}
+
+// The runs across blocks: the workgroups of the block that one begins in add up its parts, each wavefront a share of them, put together in order.
+// CHUNKS: of the chunks behind its own one, what each has of it.
+constexpr int kJoinWaves = 4;
+template <typename O, int N, bool CHUNKS>
+__global__ __launch_bounds__(kJoinWaves * 64) void join_runs_kernel(const Occurrence* __restrict__ sorted, const unsigned* __restrict__ n, int64_t width,
+                                                      const float* __restrict__ parts, int64_t part_stride, float scale,
+                                                      O* __restrict__ out, int64_t out_stride, int accumulate, unsigned first_block) {
+  __shared__ float shares[kJoinWaves][64][N + 1];   // (N + 1: lanes' numbers in different banks)
+  const unsigned block = first_block + blockIdx.x, first = block * (unsigned)kBlock, all = *n, end = first + kBlock;
+  if (end >= all) return;
+  const unsigned token = sorted[end - 1].token;
+  if (sorted[end].token != token) return;
+  if (sorted[first].token == token && first > 0 && sorted[first - 1].token == token) return;   // (it begins further in front)
+  // the last block that has some of it (its tokens begin blocks up to there)
+  const unsigned next = block + 1, last = last_block_of(token, sorted, next, (all - 1) / kBlock);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t column = ((int64_t)blockIdx.y * 64 + lane) * N;
+  const bool live = column < width;
+  const int64_t c = live ? column : 0;
+  float sum[N] = {};
+  auto add = [&](unsigned at, unsigned step, unsigned count) {   // parts of blocks at, at + step, ...: a share for each wavefront
+    const unsigned share = (count + kJoinWaves - 1) / kJoinWaves, begin = min(wave * share, count);
+    sum_parts<N>(parts + 2 * ((int64_t)at + (int64_t)begin * step) * part_stride + c, 2 * (int64_t)step * part_stride, min(share, count - begin), sum);
+  };
+  if (!CHUNKS) {
+    add(next, 1, last - block);
+  } else {
+    const unsigned chunk = (next + kChunk - 1) / kChunk;   // the first one that it comes into
+    add(next, 1, min(last + 1, chunk * kChunk) - next);
+    if (last >= chunk * kChunk) add(chunk * kChunk, kChunk, last / kChunk - chunk + 1);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) shares[wave][lane][i] = sum[i];
+  __syncthreads();
+  if (wave || !live) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum[i] = parts[(2 * (int64_t)block + 1) * part_stride + c + i];
+#pragma unroll
+  for (int w = 0; w < kJoinWaves; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] += shares[w][lane][i];
   put_sum<O, N>(out + (int64_t)token * out_stride, sum, scale, accumulate, c, width);
 }
 
@@ -453,6 +505,9 @@ int row_lanes_shift(int64_t vectors) {
   while (shift < 8 && (1ll << shift) < vectors) ++shift;
   return shift;
 }
+
+// From here on chunks are summed in a launch of their own.
+constexpr int64_t kManyBlocks = 1024;
 
 struct GradWorkspace {
   size_t sorted[2], counts, parts, total, bytes;
@@ -584,7 +639,17 @@ int fpsched_op_embedding_grad(int device_id, int type, const void* grad, int64_t
             const dim3 blocks((unsigned)w.blocks, (unsigned)ceil_div(width, 64 * N));
             row_sums_kernel<T, O, N><<<blocks, dim3(64), 0, stream>>>(static_cast<const T*>(grad), grad_stride, width, sorted, total, scale,
                                                                       static_cast<O*>(out), out_stride, accumulate, parts, w.part_stride);
-            join_runs_kernel<O, N><<<blocks, dim3(64), 0, stream>>>(sorted, total, width, parts, w.part_stride, scale, static_cast<O*>(out), out_stride, accumulate);
+            auto join = [&](auto chunks) {
+              for (int64_t at = 0; at < w.blocks; at += kMostGroups)
+                join_runs_kernel<O, N, decltype(chunks)::value><<<dim3((unsigned)std::min(kMostGroups, w.blocks - at), blocks.y), dim3(kJoinWaves * 64), 0, stream>>>(
+                    sorted, total, width, parts, w.part_stride, scale, static_cast<O*>(out), out_stride, accumulate, (unsigned)at);
+            };
+            if (w.blocks > kManyBlocks) {
+              chunk_sums_kernel<N><<<dim3((unsigned)ceil_div(w.blocks, kChunk), blocks.y), dim3(64), 0, stream>>>(sorted, total, width, parts, w.part_stride);
+              join(std::true_type());
+            } else {
+              join(std::false_type());
+            }
           }
           return launched();
         };

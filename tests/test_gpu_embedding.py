@@ -141,3 +141,26 @@ def test_lookup_of_more_rows_than_a_grid_has_workgroups():
         at = tokens[first:first + 100].long()
         want = torch.where(((at >= 0) & (at < 1000))[:, None], table[at.clamp(0, 999)], 0)
         assert torch.equal(got[first:first + 100], want), first
+
+
+@pytest.mark.parametrize("repeat", [0.0, 0.3, 0.75])
+@pytest.mark.parametrize("n,rows,width", [(16384, 500, 8), (16385, 70000, 3), (20000, 40, 24), (70000, 300, 8), (300000, 100000, 2), (140000, 1, 9)])
+def test_gradient_of_many_tokens(n, rows, width, repeat):
+    # (runs of a few tokens and of most of them, over several chunks of blocks; more tokens than one workgroup sorts)
+    g = torch.Generator().manual_seed(n + rows)
+    grad, tokens = torch.randn(n, width, generator=g), tokens_of(n, rows, n + 1, repeat)
+    for dtype in (torch.bfloat16, torch.float32):
+        got = ops.embedding_grad(grad.to(dtype).cuda(), tokens.cuda(), rows)
+        oracle.assert_near(got, *oracle.embedding_grad(grad.to(dtype), tokens, rows, 1.0, dtype), str(dtype))
+        assert torch.equal(got, ops.embedding_grad(grad.to(dtype).cuda(), tokens.cuda().int(), rows))
+
+
+def test_gradient_of_one_run_exactly():
+    # (whole numbers, whose sums have no rounding: every length up to and over the ends of blocks and of chunks of blocks)
+    for n in (1, 15, 16, 17, 1023, 1024, 1025, 16383, 16384, 16400, 17407, 17408, 17409, 33000, 66000):
+        for front in (0, 5, 16, 1024):
+            tokens = torch.cat([torch.zeros(front, dtype=torch.int32), torch.ones(n, dtype=torch.int32), torch.full((3,), 2, dtype=torch.int32)]).cuda()
+            grad = (torch.arange(n + front + 3, device="cuda") % 7 - 3).float()[:, None].expand(-1, 8).contiguous()
+            got = ops.embedding_grad(grad, tokens, 4)
+            want = torch.stack([grad[:front].sum(0), grad[front:front + n].sum(0), grad[front + n:].sum(0), torch.zeros(8, device="cuda")])
+            assert torch.equal(got, want), (n, front)
