@@ -71,20 +71,28 @@ __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf
 
 constexpr float kGeluScale = 1.5957691216057308f, kGeluCube = 0.044715f;   // 2 sqrt(2 / pi); (1 + tanh y) / 2 = sigmoid(2 y)
 
-__device__ __forceinline__ float activate(int act, float g) {
-  if (act == FPSCHED_SILU) return g * sigmoid(g);
-  if (act == FPSCHED_GELU) return g * sigmoid(kGeluScale * (g + kGeluCube * g * g * g));
-  return fmaxf(g, 0.f);
-}
-__device__ __forceinline__ float slope(int act, float g) {
-  if (act == FPSCHED_RELU) return g > 0.f ? 1.f : 0.f;
-  const float c = fminf(fmaxf(g, -40.f), 40.f);   // (beyond, 0 or 1 to the last bit; squares would overflow)
-  if (act == FPSCHED_SILU) {
-    const float p = sigmoid(c);
-    return p * (1.f + c * (1.f - p));
+// act(g) and act'(g).  Of |g| beyond 40 the sigmoid is 0 or 1 to the last bit of what it is added to, and what else the derivative has of g is held there (squares
+// would overflow, and 0 times infinity is none).
+template <int ACT>
+struct Activation {
+  float value, slope;
+  __device__ __forceinline__ explicit Activation(float g) {
+    if constexpr (ACT == FPSCHED_RELU) {
+      value = g < 0.f ? 0.f : g;   // (and none of what is none)
+      slope = g > 0.f ? 1.f : 0.f;
+    } else {
+      const float p = sigmoid(ACT == FPSCHED_SILU ? g : kGeluScale * (g + kGeluCube * g * g * g)), c = fminf(fmaxf(g, -40.f), 40.f), rest = c * p * (1.f - p);
+      value = g * p;
+      slope = p + (ACT == FPSCHED_SILU ? rest : rest * kGeluScale * (1.f + 3.f * kGeluCube * c * c));
+    }
   }
-  const float p = sigmoid(kGeluScale * (c + kGeluCube * c * c * c));
-  return p + c * p * (1.f - p) * kGeluScale * (1.f + 3.f * kGeluCube * c * c);
+};
+// f(Activation<act>'s number): the choice is made once for all elements that a lane has, so that their exponentials do not wait one for another
+template <typename F>
+__device__ __forceinline__ void with_activation(int act, F f) {
+  if (act == FPSCHED_SILU) f(std::integral_constant<int, FPSCHED_SILU>());
+  else if (act == FPSCHED_GELU) f(std::integral_constant<int, FPSCHED_GELU>());
+  else f(std::integral_constant<int, FPSCHED_RELU>());
 }
 
 // ---- tiles in LDS --------------------------------------------------------------------------------------------------------
@@ -237,11 +245,12 @@ template <typename T, int N>
 __device__ __forceinline__ void put_gated(const Gemm& a, int64_t m, int64_t n, const Vec<float, N>& gate, const Vec<float, N>& up) {
   Vec<T, N> h;
   Kept<N> kept;
+  with_activation(a.act, [&](auto act) {
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    h.at[e] = (T)(activate(a.act, gate.at[e]) * up.at[e]);
-    if (e % 2) kept.set(e / 2, gate.at[e - 1], gate.at[e], up.at[e - 1], up.at[e]);
-  }
+    for (int e = 0; e < N; ++e) h.at[e] = (T)(Activation<decltype(act)::value>(gate.at[e]).value * up.at[e]);
+  });
+#pragma unroll
+  for (int e = 0; e < N; e += 2) kept.set(e / 2, gate.at[e], gate.at[e + 1], up.at[e], up.at[e + 1]);
   store_vec<T, N>(static_cast<T*>(a.out) + m * a.out_stride + n, h);
   if (a.kept) kept.store(a, m, n);
 }
@@ -272,13 +281,16 @@ __device__ __forceinline__ void put_columns(const Gemm& a, int64_t m, int64_t n,
   if constexpr (EPILOGUE == kGatedGrad) {
     asm volatile("" : : : "memory");   // (what is written below is of another type, in the place that `before` was read from)
     Vec<T, 8> dg, du, h;
+    with_activation(a.act, [&](auto act) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float gate = before.kept.gate(e), up = before.kept.up(e), act = activate(a.act, gate);
-      dg.at[e] = (T)(x.at[e] * up * slope(a.act, gate));
-      du.at[e] = (T)(x.at[e] * act);
-      h.at[e] = (T)(act * up);
-    }
+      for (int e = 0; e < 8; ++e) {
+        const Activation<decltype(act)::value> of(before.kept.gate(e));
+        const float up = before.kept.up(e);
+        dg.at[e] = (T)(x.at[e] * up * of.slope);
+        du.at[e] = (T)(x.at[e] * of.value);
+        h.at[e] = (T)(of.value * up);
+      }
+    });
     T* out = reinterpret_cast<T*>(Kept<8>::first_of(a, m, n));
     store_vec<T, 8>(out, dg);
     store_vec<T, 8>(out + a.n_half, du);
