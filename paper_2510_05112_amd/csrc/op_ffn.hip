@@ -309,14 +309,15 @@ __device__ __forceinline__ void put_columns(const Gemm& a, int64_t m, int64_t n,
   }
 }
 
-// All wavefronts of a workgroup have read what they read of LDS, and their loads to it have arrived.
+// All wavefronts of a workgroup have read what they read of LDS, and their loads to it have arrived but for the last ON_THEIR_WAY.
+template <int ON_THEIR_WAY = 0>
 __device__ __forceinline__ void meet() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "i"(ON_THEIR_WAY) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" : : : "memory");
 }
 
-template <typename T, int LM, int LN, int EPILOGUE, typename O, int BM, int BN, int kWavesM, int kWavesN>
+template <typename T, int LM, int LN, int EPILOGUE, typename O, int BM, int BN, int kWavesM, int kWavesN, int kPlaces>
 __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
   constexpr int kThreads = kWavesM * kWavesN * 64;
   constexpr int MF = BM / kWavesM / 32, NF = BN / kWavesN / 32, kStepsOfTile = kDepth / 16;
@@ -324,7 +325,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
   using TileM = Tile<LM, BM, kThreads, false>;
   using TileN = Tile<LN, BN, kThreads, kHalves>;
   constexpr int kTile = TileM::kBytes + TileN::kBytes;
-  __shared__ __align__(1024) char lds[2 * kTile];
+  __shared__ __align__(1024) char lds[kPlaces * kTile];
   const int thread = threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int wave_m = wave / kWavesN, wave_n = wave % kWavesN;
   int tm, tn;
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
   // (That the two places are different ones is said by __restrict: the compiler would else wait for what is on its way to one in front of
   // each transposing read of the other.)
   auto work_on = [&](int t, lds_char* __restrict place, lds_char* __restrict other) __attribute__((always_inline)) {
-    next_tile(t + 1);
+    next_tile(t + kPlaces - 1);
 #pragma unroll
     for (int step = 0; step < kStepsOfTile; ++step) {
       const int to = step & 1, of = to ^ 1;   // fragments to read, to multiply (in the first tile's first step, zeros)
@@ -385,12 +386,15 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
     }
   };
   lds_char* const room = (lds_char*)lds;
-  next_tile(0);
 #pragma unroll
-  for (int l = 0; l < kLoads; ++l) load(room, l);
+  for (int p = 0; p < kPlaces - 1; ++p) {
+    next_tile(p);
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) load(room + p * kTile, l);
+  }
   for (int t = 0; t < tiles; ++t) {
-    meet();
-    work_on(t, room + (t & 1) * kTile, room + ((t + 1) & 1) * kTile);
+    meet<kLoads * (kPlaces - 2)>();
+    work_on(t, room + t % kPlaces * kTile, room + (t + kPlaces - 1) % kPlaces * kTile);
   }
 #pragma unroll
   for (int i = 0; i < MF; ++i)
@@ -400,7 +404,7 @@ __global__ __launch_bounds__(kWavesM * kWavesN * 64) void gemm_kernel(Gemm a) {
   constexpr int kPad = NF * 32 + 4;   // floats between rows: 16 rows' pieces of 16 bytes are in different banks
   meet();   // (the loads of the tile behind the last one, zeros, among them)
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * kPad;
-  static_assert(kThreads / 64 * 32 * kPad * 4 <= 2 * kTile, "the rows fit");
+  static_assert(kThreads / 64 * 32 * kPad * 4 <= kPlaces * kTile, "the rows fit");
   constexpr int kColumns = (kHalves ? NF / 2 : NF) * 32, kLanes = kColumns / 8, kRows = 64 / kLanes;   // of the output; lanes of a row, rows at a time
   const int64_t n = n0 + wave_n * kColumns + lane % kLanes * 8;
   // What is read there is on its way 32 rows ahead.  (Read where it is needed, one wait after another: the gate's gradient of 8,192 x 10,752 x 4,096
@@ -578,11 +582,14 @@ __global__ __launch_bounds__(256) void add_shares_kernel(Gemm a) {
 // How a product is cut: into tiles of 256 x 256, one workgroup to a compute unit, or of 128 x 128, two of them; and the tiles
 // of the last round, where they leave compute units idle, into shares of k, whose sums another kernel adds up.  What decides is an estimate:
 // a step of 64 k takes 1.63 us and what becomes of a tile 5 (of the gate's gradient 30: it reads and writes 0.8 MB a tile); of the small tiles 1.1 us, 0.65 with one workgroup to a compute
-// unit, and 3; sums are written and read at 8 TB/s, in a launch more.  (Measured, whole and so: W of
+// unit (a fifth less with four places; counted so, cuts were no better), and 3; sums are written and read at 8 TB/s, in a launch more.  (Measured, whole and so: W of
 // 8,192 x 4,096 x 10,752, whose 1,344 tiles are five rounds and a quarter, 1.80 and 1.69 ms; d_x of 509 x 2,560 x 6,912, 80 small tiles of 216 steps, 134
 // and 45 us.)
 struct Split {
   bool large;
+  // Small tiles, one to a compute unit, of eight steps or more: four places in LDS instead of two, so that three tiles of loads are on their way (F of 200 x
+  // 2,560 x 6,912 42 us instead of 50, B of 509 73 instead of 79; with one to four steps a kernel takes a microsecond more).
+  bool deep;
   int tiles_m, tiles_n, whole, parts;
   int64_t part_depth;
 };
@@ -603,7 +610,7 @@ Split split(int64_t m, int64_t n, int64_t depth, bool heavy) {
                         (used > 1 ? 4 + end + rest * used * (std::min(m, side) * side * 8 / 8e6) : 0);
       if (least == 0 || us < least) {
         least = us;
-        best = {large, (int)std::min<int64_t>(tm, INT32_MAX), (int)std::min<int64_t>(tn, INT32_MAX), (int)std::min<int64_t>(used > 1 ? tiles - rest : tiles, INT32_MAX), (int)used, each * kDepth};
+        best = {large, !large && tiles - rest + rest * used <= 256 && each >= 8, (int)std::min<int64_t>(tm, INT32_MAX), (int)std::min<int64_t>(tn, INT32_MAX), (int)std::min<int64_t>(used > 1 ? tiles - rest : tiles, INT32_MAX), (int)used, each * kDepth};
       }
     }
   }
@@ -631,10 +638,11 @@ int gemm(Gemm a, void* workspace, hipStream_t stream) {
   const dim3 grid(s.whole + shared * s.parts);
   constexpr int kHalf = EPILOGUE == kGated ? 2 : 1;
   if (s.large) {
-    gemm_kernel<T, LM, LN, EPILOGUE, O, 256, 256, 2, 4><<<grid, dim3(512), 0, stream>>>(a);
+    gemm_kernel<T, LM, LN, EPILOGUE, O, 256, 256, 2, 4, 2><<<grid, dim3(512), 0, stream>>>(a);
     if (shared) add_shares_kernel<T, EPILOGUE, O, 256><<<dim3(shared * 32 / kHalf), dim3(256), 0, stream>>>(a);
   } else {
-    gemm_kernel<T, LM, LN, EPILOGUE, O, 128, 128, 2, 2><<<grid, dim3(256), 0, stream>>>(a);
+    if (s.deep) gemm_kernel<T, LM, LN, EPILOGUE, O, 128, 128, 2, 2, 4><<<grid, dim3(256), 0, stream>>>(a);
+    else gemm_kernel<T, LM, LN, EPILOGUE, O, 128, 128, 2, 2, 2><<<grid, dim3(256), 0, stream>>>(a);
     if (shared) add_shares_kernel<T, EPILOGUE, O, 128><<<dim3(shared * 8 / kHalf), dim3(256), 0, stream>>>(a);
   }
   return launched();
