@@ -164,3 +164,24 @@ def test_gradient_of_one_run_exactly():
             got = ops.embedding_grad(grad, tokens, 4)
             want = torch.stack([grad[:front].sum(0), grad[front:front + n].sum(0), grad[front + n:].sum(0), torch.zeros(8, device="cuda")])
             assert torch.equal(got, want), (n, front)
+
+
+@pytest.mark.parametrize("n,rows,width,apart", [(5000, 300000, 128, 0), (16384, 300007, 129, 0), (37, 300001, 130, 3), (3000, 70000, 512, 8)])
+def test_gradient_of_a_large_table(n, rows, width, apart):
+    # (zeros are most of the work: with tokens close together around a quarter of the table, and everywhere)
+    g = torch.Generator().manual_seed(n)
+    tokens = tokens_of(n, rows, n + 1)
+    between = rows // 4 // 16 * 16
+    near = torch.rand(n, generator=g) < 0.2
+    tokens[near] = between + torch.randint(-3, 3, (int(near.sum()),), generator=g)
+    grad = torch.randn(n, width, generator=g).bfloat16()
+    for out_dtype in (torch.bfloat16, torch.float32):
+        store = torch.full((rows, width + apart), 5.0, dtype=out_dtype, device="cuda")
+        got = ops.embedding_grad(grad.cuda(), tokens.cuda(), rows, out=store[:, :width])
+        ids, at = torch.unique(tokens[(tokens >= 0) & (tokens < rows)], return_inverse=True)
+        small = torch.full((n,), -1)
+        small[(tokens >= 0) & (tokens < rows)] = at
+        oracle.assert_near(got[ids.cuda()], *oracle.embedding_grad(grad, small, len(ids), 1.0, out_dtype))
+        without = torch.ones(rows, dtype=torch.bool)
+        without[ids] = False
+        assert bool((got[without.cuda()] == 0).all()) and bool((store[:, width:] == 5).all())
