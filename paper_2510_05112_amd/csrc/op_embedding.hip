@@ -113,26 +113,28 @@ __device__ __forceinline__ unsigned long long same_digit(bool have, unsigned dig
 }
 __device__ __forceinline__ unsigned lanes_in_front(unsigned long long of, int lane) { return __popcll(of & ((1ull << lane) - 1)); }
 
-// Up to kOneSort occurrences, all passes by one workgroup in LDS.  A wavefront has 64 `rounds` adjacent ones; a lane's place among those
+// Up to kOneSort occurrences, all passes by one workgroup in LDS, ROUNDS of 1,024 (as many as there are: with room for 16, 4,000 tokens took 28.6 us
+// into a table of 5,000 x 512, and 22.7 with room for 4).  A wavefront has 64 `rounds` adjacent ones; a lane's place among those
 // of its digit is counted wavefront by wavefront, then over the wavefronts, then over the digits.
 constexpr unsigned kNone = ~0u;   // (a table has fewer rows)
-constexpr int kOneRounds = 16, kOneSort = 1024 * kOneRounds;
+constexpr int kMostRounds = 16, kOneSort = 1024 * kMostRounds;
 
+template <int ROUNDS>
 __global__ __launch_bounds__(1024) void sort_few_kernel(const void* tokens, int tokens64, int n_tokens, int64_t n_rows, Occurrence* sorted,
                                                        unsigned* total, Fill fill) {
   if (fill.mine()) return fill.run();
-  __shared__ unsigned held_token[kOneSort];
-  __shared__ unsigned short held_at[kOneSort];
+  __shared__ unsigned held_token[1024 * ROUNDS];
+  __shared__ unsigned short held_at[1024 * ROUNDS];
   __shared__ unsigned short next[16][kDigits];
   __shared__ unsigned sums[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int rounds = (n_tokens + 1023) / 1024;
   int n = n_tokens;
   for (int shift = 0; shift == 0 || (n_rows - 1) >> shift != 0; shift += 8) {
-    unsigned token[kOneRounds];     // kNone: none
-    unsigned at_rank[kOneRounds];   // which occurrence it is; in the upper half, its place among those of its digit
+    unsigned token[ROUNDS];     // kNone: none
+    unsigned at_rank[ROUNDS];   // which occurrence it is; in the upper half, its place among those of its digit
 #pragma unroll
-    for (int r = 0; r < kOneRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
       const int i = (wave * rounds + r) * 64 + lane;
       token[r] = kNone, at_rank[r] = 0;
       if (r < rounds && i < n) {
@@ -147,7 +149,7 @@ __global__ __launch_bounds__(1024) void sort_few_kernel(const void* tokens, int 
     for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) next[0][i] = 0;
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kOneRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
       if (r < rounds) {
         const bool have = token[r] != kNone;
         const unsigned digit = token[r] >> shift & (kDigits - 1);
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(1024) void sort_few_kernel(const void* tokens, int 
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kOneRounds; ++r)
+    for (int r = 0; r < ROUNDS; ++r)
       if (token[r] != kNone) {
         const unsigned place = next[wave][token[r] >> shift & (kDigits - 1)] + (at_rank[r] >> 16);
         held_token[place] = token[r];
@@ -603,10 +605,18 @@ int fpsched_op_embedding_grad(int device_id, int type, const void* grad, int64_t
     return dim3((unsigned)(groups + fillers));
   };
   const Occurrence* sorted = reinterpret_cast<const Occurrence*>(base + w.sorted[0]);
-  if (n_tokens <= kOneSort) {
+  // (Of more than 8,192 one workgroup takes longer than many in several launches, 57 and 45 us for 16,000 tokens into 5,000 x 512, but where it is done before
+  // the zeros are, those go faster in one launch: 281 and 324 us for 16,384 into 262,144 x 2,560, 55 and 71 for 8,300 into 70,000 x 512 of 32 bits.)
+  const bool many_zeros = fill.out && n_rows * width * out_size >= 64 << 20;
+  if (n_tokens <= (many_zeros ? kOneSort : kOneSort / 2)) {
     fill.slices = 1;
     const dim3 groups = grid(1, 1024);
-    sort_few_kernel<<<groups, dim3(1024), 0, stream>>>(tokens, tokens64, (int)n_tokens, n_rows, reinterpret_cast<Occurrence*>(base + w.sorted[0]), total, fill);
+    auto sort = [&](auto rounds) {
+      sort_few_kernel<decltype(rounds)::value><<<groups, dim3(1024), 0, stream>>>(tokens, tokens64, (int)n_tokens, n_rows, reinterpret_cast<Occurrence*>(base + w.sorted[0]), total, fill);
+    };
+    if (n_tokens <= 1024 * 4) sort(std::integral_constant<int, 4>());
+    else if (n_tokens <= 1024 * 8) sort(std::integral_constant<int, 8>());
+    else sort(std::integral_constant<int, kMostRounds>());
   } else {
     int passes = 1;
     while ((n_rows - 1) >> 8 * passes) ++passes;

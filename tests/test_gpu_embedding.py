@@ -185,3 +185,13 @@ def test_gradient_of_a_large_table(n, rows, width, apart):
         without = torch.ones(rows, dtype=torch.bool)
         without[ids] = False
         assert bool((got[without.cuda()] == 0).all()) and bool((store[:, width:] == 5).all())
+
+
+@pytest.mark.parametrize("n", [4095, 4096, 4097, 8191, 8192, 8193])
+def test_gradient_where_the_sort_changes(n):
+    tokens = tokens_of(n, 3000, n)
+    grad = torch.randn(n, 16, generator=torch.Generator().manual_seed(n)).half()
+    for out_dtype in (torch.float16, torch.float32):
+        out = torch.zeros(3000, 16, dtype=out_dtype, device="cuda")
+        got = ops.embedding_grad(grad.cuda(), tokens.cuda(), 3000, 0.5, out=out, accumulate=out_dtype == torch.float32)
+        oracle.assert_near(got, *oracle.embedding_grad(grad, tokens, 3000, 0.5, out_dtype))
