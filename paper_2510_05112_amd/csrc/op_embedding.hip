@@ -11,8 +11,9 @@
 // workgroups of its own; a run inside one block is written where it belongs, one across blocks leaves its parts (32 bits) in the workspace, which
 // another kernel adds up, of more than 16,384 tokens with sums over chunks of 64 blocks in between (131,072 tokens that are all the same, 1,024 wide: 767 us
 // by one wavefront a run, 193 so).  Most rows of a large vocabulary have no token: all are filled with zeros by what the sort leaves of the chip.
-// Floor: grad read once, dE written once.  Measured (bf16): 4,096 tokens into 65,536 x 4,096 sort and zeros 89 us (537 MB of zeros: 6.1 TB/s,
-// and a fill by itself reaches 6.9), sums 25, runs across blocks 8; 16,384 into 262,144 x 2,560 225 us, 46 and 11.
+// Floor: grad read once, dE written once.  Measured (bf16): 4,096 tokens into 65,536 x 4,096 sort and zeros 88 us (537 MB of zeros: 6.1 TB/s,
+// and a fill by itself reaches 6.9), sums 25, runs across blocks 7; 16,384 into 262,144 x 2,560 224 us, 47 and 8.  (Zeros of some rows beside the sums of
+// others instead, a quarter of the table: 134 against 119 us and 302 against 290.)
 #include "ops_common.h"
 
 #include <algorithm>

@@ -12,8 +12,8 @@
 //
 // The N operand is the matrix instruction's first, so that a lane holds four neighbouring n of one m, which is how rows are written.
 //
-// Measured, bf16 8,192 x 4,096 x 10,752 (in PFLOP/s; a large library product 1.1 to 1.6): x w_in^T 1.17, hidden w_out^T 1.30, grad w_out 0.92 (it
-// moves 1.06 GB of kept numbers and gradients besides, 215 us of 787), d_pre w_in 1.34, d_pre^T x 1.28, grad^T hidden 1.20, with the sums of shared tiles.  The
+// Measured, bf16 8,192 x 4,096 x 10,752 (in PFLOP/s; a large library product 1.1 to 1.6): x w_in^T 1.17, hidden w_out^T 1.28, grad w_out 0.97 (it
+// moves 1.06 GB of kept numbers and gradients besides, 215 us of 747), d_pre w_in 1.34, d_pre^T x 1.28, grad^T hidden 1.20, with the sums of shared tiles.  The
 // matrix cores are busy two thirds of the time at 1.7 GHz: the card's power bounds it.
 #include "ops_common.h"
 

@@ -5,7 +5,7 @@
 // and two parts of a row are put together by multiplying s by e^(m1 - m) and adding s (m1 - m) to w.  A lane looks at 16
 // bytes of logits at a time and changes its m only where one of them is larger.  Rows are cut into parts where there are fewer rows than
 // the chip has room for; a second kernel puts the parts together.  Bound by memory for many rows (4,096 x 65,536 bf16: 105 us, 5.1 TB/s), for few by
-// ten instructions a logit and by what each part costs beside its logits (61 x 262,144: 14.8 us and 4.9 for the parts).
+// ten instructions a logit and by what each part costs beside its logits (61 x 262,144: 15.5 us and 4.9 for the parts).
 //
 // Alternatives: of 32 groups of lanes each has a largest logit, and k logits at least are
 // not below the k-th of these, the bar; each lane knows the largest of each of its pieces, and the pieces with one that is not below the bar are
