@@ -83,9 +83,11 @@ __device__ __forceinline__ Stats wave_stats(Stats a) {
   a.w = over_lanes(a.w, add);
   return a;
 }
-// The sums of kWaves wavefronts, by each lane.
+// The sums of WAVES wavefronts, by each lane.
+template <int WAVES>
 __device__ __forceinline__ Stats put_together(const Stats* wave_sums, int lane) {
-  static_assert(kWaves == 4, "the lanes are taken in fours");
+  static_assert(WAVES == 1 || WAVES == 4, "the lanes are taken in fours");
+  if (WAVES == 1) return wave_sums[0];
   Stats a = wave_sums[lane & 3];
   float most = fmaxf(a.m, across<1>(a.m));
   a.raise(fmaxf(most, across<2>(most)));
@@ -117,6 +119,7 @@ __device__ __forceinline__ unsigned long long wave_most(unsigned long long a) {
 constexpr int kGroups = 32;   // of the lanes of one number modulo 32: neighbouring logits are in different ones, and a part of 256 has some in each
 static_assert(kMostAlternatives <= kGroups, "as many groups of lanes as alternatives");
 constexpr int kRoom = 512;   // candidates in LDS
+constexpr int kDigits = 256;
 
 // put(place, candidate) if the at-th of n distinct candidates in LDS is one of the k largest.
 template <typename P>
@@ -180,14 +183,14 @@ struct RowOut {
   }
 };
 
-// One part of a row.  blockIdx.x: row * parts + part.  ALT: with alternatives, of at most kHeldPart logits.
-template <typename T, bool ALT>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
-  constexpr int N = kWide<T>;
-  __shared__ Stats wave_sums[kWaves];
+// One part of a row, by WAVES wavefronts.  blockIdx.x: row * parts + part.  ALT: with alternatives, of at most kHeld logits a lane.
+template <typename T, bool ALT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, sizeof(T) == 4 ? 5 : 6) void logprobs_kernel(RowOut<T> row_out, PartOut part_out, int64_t part_length) {
+  constexpr int N = kWide<T>, kLanes = WAVES * 64;
+  __shared__ Stats wave_sums[WAVES];
   __shared__ unsigned long long candidates[ALT ? kRoom : 1];
   __shared__ struct { unsigned digit, count, larger; } chosen;
-  __shared__ unsigned group_tops[ALT ? kWaves : 1][kGroups];
+  __shared__ unsigned group_tops[ALT ? WAVES : 1][kGroups];
   __shared__ int collected;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = row_out.k;
   const int64_t row = blockIdx.x / part_out.parts, part = blockIdx.x % part_out.parts;
@@ -230,15 +233,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_ker
   if constexpr (ALT) {
     Vec<T, N> v[kPieces];
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) v[p] = get(mine_at + p * kThreads * N);
+    for (int p = 0; p < kPieces; ++p) v[p] = get(mine_at + p * kLanes * N);
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) tops[p] = (unsigned)(p * kThreads * N) < length ? take(v[p]) : -INFINITY;
+    for (int p = 0; p < kPieces; ++p) tops[p] = (unsigned)(p * kLanes * N) < length ? take(v[p]) : -INFINITY;
   } else {
     constexpr int kAhead = 4;
-    for (unsigned at = mine_at; at < length; at += kAhead * kThreads * N) {
+    for (unsigned at = mine_at; at < length; at += kAhead * kLanes * N) {
       Vec<T, N> v[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) v[i] = get(at + i * kThreads * N);
+      for (int i = 0; i < kAhead; ++i) v[i] = get(at + i * kLanes * N);
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) take(v[i]);
     }
@@ -258,7 +261,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_ker
   if constexpr (ALT) {
     unsigned mine_of_groups = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) mine_of_groups = max(mine_of_groups, group_tops[w][lane & (kGroups - 1)]);
+    for (int w = 0; w < WAVES; ++w) mine_of_groups = max(mine_of_groups, group_tops[w][lane & (kGroups - 1)]);
     int larger = 0;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) larger += (unsigned)__builtin_amdgcn_readlane(mine_of_groups, g) > mine_of_groups;
@@ -277,7 +280,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_ker
     };
     if (wave == 0) collect(x_outer, outer);
     for (; again; again &= again - 1) {
-      const unsigned at = mine_at + __builtin_ctz(again) * kThreads * N;
+      const unsigned at = mine_at + __builtin_ctz(again) * kLanes * N;
       const Vec<T, N> v = get(at);
 #pragma unroll
       for (int i = 0; i < N; ++i) collect((float)v.at[i], inner + at + i);
@@ -291,21 +294,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_ker
           if (x > -INFINITY) f(ranked(x + 0.f, (unsigned)id));
         };
         if (wave == 0) one(x_outer, outer);
-        for (unsigned at = mine_at; at < length; at += kThreads * N) {
+        for (unsigned at = mine_at; at < length; at += kLanes * N) {
           const Vec<T, N> v = get(at);
 #pragma unroll
           for (int i = 0; i < N; ++i) one((float)v.at[i], inner + at + i);
         }
       };
       unsigned* counts = reinterpret_cast<unsigned*>(candidates);
-      static_assert(kThreads == 256 && (!ALT || sizeof(candidates) >= kThreads * 4), "a digit a lane");
-      const unsigned long long largest = ranked(put_together(wave_sums, lane).m + 0.f, (unsigned)begin), smallest = ranked(bar, (unsigned)(end - 1));
+      static_assert(!ALT || sizeof(candidates) >= kDigits * 4, "they fit");
+      const unsigned long long largest = ranked(put_together<WAVES>(wave_sums, lane).m + 0.f, (unsigned)begin), smallest = ranked(bar, (unsigned)(end - 1));
       int shift = (63 - __builtin_clzll((largest ^ smallest) | 1)) & ~7;
       unsigned long long known = shift == 56 ? 0 : largest >> (shift + 8) << (shift + 8);
       unsigned wanted = k;   // of those that begin with what is known
       for (; shift >= 0; shift -= 8) {
         __syncthreads();
-        counts[threadIdx.x] = 0;
+        for (int d = threadIdx.x; d < kDigits; d += kLanes) counts[d] = 0;
         __syncthreads();
         all_of_part([&](unsigned long long r) {
           if (shift == 56 || (r ^ known) >> (shift + 8) == 0) {
@@ -319,10 +322,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_ker
           }
         });
         __syncthreads();
-        unsigned larger = 0;
-        for (int d = kThreads - 1; d >= 0; --d) larger += d > (int)threadIdx.x ? counts[d] : 0u;
-        const unsigned count = counts[threadIdx.x];
-        if (larger < wanted && larger + count >= wanted) chosen = {threadIdx.x, count, larger};
+        for (int digit = threadIdx.x; digit < kDigits; digit += kLanes) {
+          unsigned larger = 0;
+          for (int d = kDigits - 1; d >= 0; --d) larger += d > digit ? counts[d] : 0u;
+          const unsigned count = counts[digit];
+          if (larger < wanted && larger + count >= wanted) chosen = {(unsigned)digit, count, larger};
+        }
         __syncthreads();
         known |= (unsigned long long)chosen.digit << shift;
         wanted -= chosen.larger;
@@ -338,7 +343,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_ker
   }
   const bool whole = part_out.parts == 1;
   const int64_t at = row * part_out.parts + part;
-  const Stats all = whole || wave == 0 ? put_together(wave_sums, lane) : nothing();
+  const Stats all = whole || wave == 0 ? put_together<WAVES>(wave_sums, lane) : nothing();
   if (threadIdx.x == 0) {
     if (whole) row_out.put(row, all, given, is_given);
     else part_out.stats[at] = all;
@@ -349,7 +354,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 5 : 6) void logprobs_ker
       if (whole) row_out.put_alternative(row, i, r, all);
       else part_out.best[at * k + i] = r;
     };
-    for (int first = wave * 64; first < n; first += kThreads) by_rank(candidates, n, k, first + lane, put);
+    for (int first = wave * 64; first < n; first += kLanes) by_rank(candidates, n, k, first + lane, put);
     if ((int)threadIdx.x >= n && (int)threadIdx.x < k) put(threadIdx.x, 0);
   }
 }
@@ -472,6 +477,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(const T* logits
   }
 }
 
+// Rows that one wavefront takes, of more than kFewRows (4,096 x 4,000 bf16: 9.9 us, and 14.0 by four wavefronts a row; 4,096 x 1,500 f16, k 20: 12.1 and 18.3;
+// but 300 x 3,000 f32, k 4: 7.1 and 6.3).
+constexpr int64_t kShortRow = 4096, kFewRows = 512;
+static_assert(kShortRow <= 64 * kHeld, "a wavefront holds a short row");
+
 struct Parts {
   int64_t length;
   int parts;
@@ -535,8 +545,13 @@ int fpsched_op_logprobs(int device_id, int type, int64_t n_rows, int64_t vocab, 
     for (int64_t at = 0; at < n_rows; at += most) {
       const int64_t n = std::min(most, n_rows - at);
       const dim3 grid((unsigned)(n * p.parts));
-      if (n_alternatives > 0) logprobs_kernel<T, true><<<grid, dim3(kThreads), 0, stream>>>(row, part, p.length);
-      else logprobs_kernel<T, false><<<grid, dim3(kThreads), 0, stream>>>(row, part, p.length);
+      auto go = [&](auto waves) {
+        constexpr int W = decltype(waves)::value;
+        if (n_alternatives > 0) logprobs_kernel<T, true, W><<<grid, dim3(W * 64), 0, stream>>>(row, part, p.length);
+        else logprobs_kernel<T, false, W><<<grid, dim3(W * 64), 0, stream>>>(row, part, p.length);
+      };
+      if (vocab <= kShortRow && n_rows > kFewRows) go(std::integral_constant<int, 1>());
+      else go(std::integral_constant<int, kWaves>());
       if (p.parts > 1) logprobs_join_kernel<T><<<dim3((unsigned)n), dim3(kThreads), 0, stream>>>(row, part);
       row = row.behind(n);
     }
