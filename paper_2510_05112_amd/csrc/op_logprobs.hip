@@ -442,6 +442,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(RowOut<T> row_o
   }
 }
 
+constexpr int kGradRounds = 4;
 template <typename T, int N>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(const T* logits, int64_t stride, int64_t vocab, const void* tokens,
                                                                 int tokens64, const float* lse, const float* entropy,
@@ -455,24 +456,30 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(const T* logits
   const T* from = logits + row * stride;
   T* to = out + row * out_stride;
   const bool none = ln == -INFINITY;
-  auto gradient = [&](T x, int64_t i) {
+  auto gradient = [&](T x, bool is_token) {
     const float lp = ((float)x - m) - ln;
     const float p = fast_exp(lp);
-    const float d = (i == token ? gl : 0.f) - p * (gl + ge * (held_back(lp) + h));
+    const float d = (is_token ? gl : 0.f) - p * (gl + ge * (held_back(lp) + h));
     return (T)(none ? 0.f : d);
   };
-  constexpr int kRounds = 4;
-  const int64_t first = ((int64_t)(blockIdx.x % pieces) * kRounds * kThreads + threadIdx.x) * N;
+  // pieces of 16 bytes that are aligned as such, and up to N - 1 elements in front of them and behind them, by the row's first workgroup
+  const unsigned piece = blockIdx.x % pieces;
+  const int64_t inner = N == 1 ? 0 : min((int64_t)((0 - reinterpret_cast<uintptr_t>(from)) % 16 / sizeof(T)), vocab), length = (vocab - inner) / N * N;
+  if (N > 1 && piece == 0 && threadIdx.x < 2 * N) {
+    const int64_t i = threadIdx.x < N ? threadIdx.x : inner + length + threadIdx.x - N;
+    if (threadIdx.x < N ? i < inner : i < vocab) to[i] = gradient(from[i], i == token);
+  }
+  const int64_t first = ((int64_t)piece * kGradRounds * kThreads + threadIdx.x) * N;
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
+  for (int r = 0; r < kGradRounds; ++r) {
     const int64_t c = first + (int64_t)r * kThreads * N;
-    if (c + N <= vocab) {
-      Vec<T, N> v = load_vec<T, N>(from + c);
+    if (c < length) {
+      Vec<T, N> v = load_vec<T, N>(from + inner + c);
+      const int64_t behind = token - inner - c;
+      const int at = behind >= 0 && behind < N ? (int)behind : -1;   // the token's place in the piece
 #pragma unroll
-      for (int i = 0; i < N; ++i) v.at[i] = gradient(v.at[i], c + i);
-      store_vec<T, N>(to + c, v);
-    } else {
-      for (int64_t i = c; i < vocab; ++i) to[i] = gradient(from[i], i);
+      for (int i = 0; i < N; ++i) v.at[i] = gradient(v.at[i], i == at);
+      store_vec<T, N>(to + inner + c, v);
     }
   }
 }
@@ -574,7 +581,7 @@ int fpsched_op_logprobs_grad(int device_id, int type, int64_t n_rows, int64_t vo
     using T = decltype(zero);
     auto go = [&](auto n) {
       constexpr int N = decltype(n)::value;
-      const int64_t pieces = ceil_div(vocab, 4 * kThreads * N);
+      const int64_t pieces = ceil_div(vocab, kGradRounds * kThreads * N);
       const int64_t most = kMostGroups / pieces;   // rows of a launch
       for (int64_t at = 0; at < n_rows; at += most)
         logprobs_grad_kernel<T, N><<<dim3((unsigned)(std::min(most, n_rows - at) * pieces)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
@@ -582,7 +589,9 @@ int fpsched_op_logprobs_grad(int device_id, int type, int64_t n_rows, int64_t vo
             out_stride, (int)pieces, at);
       return launched();
     };
-    if (wide_rows(logits, logits_stride, sizeof(T)) && wide_rows(out, out_stride, sizeof(T))) return go(std::integral_constant<int, kWide<T>>());
+    // (rows of both at the same distance from a multiple of 16 bytes: 509 x 100,003 f16 34 us, and 56 an element a lane)
+    const auto apart = reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(out);
+    if (apart % 16 == 0 && (logits_stride - out_stride) * (int64_t)sizeof(T) % 16 == 0) return go(std::integral_constant<int, kWide<T>>());
     return go(std::integral_constant<int, 1>());
   });
 }
