@@ -1,7 +1,6 @@
 // Embedding lookup of a model's first stage, and the gradient of its table.
 //
-// Lookup: out[t] = scale table[tokens[t]].  A row is moved by a power of two of lanes, 16 bytes a lane where rows are
-// 16-byte aligned (else an element a lane); bound by memory for many tokens, by one load behind another (token, row) for few: 61 rows of
+// Lookup: out[t] = scale table[tokens[t]].  A row is moved by a power of two of lanes, 16 bytes a lane, whatever its address; bound by memory for many tokens, by one load behind another (token, row) for few: 61 rows of
 // 2,560 take 2.8 us.
 //
 // Gradient: dE[v] = scale sum over {t : tokens[t] = v} grad[t].  Adding rows with atomics would make the sums depend on
@@ -26,10 +25,11 @@ constexpr int64_t kMaxWidth = 1 << 20, kMaxSummed = 1 << 30;   // (what the grid
 
 // ---- lookup ----------------------------------------------------------------------------------------------------------
 
-template <typename T, int N>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void embedding_kernel(const T* table, int64_t table_stride, int64_t n_rows, int64_t width,
                                                             const void* tokens, int tokens64, int64_t n_tokens, float scale, T* out,
                                                             int64_t out_stride, int lanes_shift) {
+  constexpr int N = kWide<T>;
   const int64_t step = (int64_t)gridDim.x << (8 - lanes_shift);   // (more than one each where a grid has no room for all)
   for (int64_t t = ((int64_t)blockIdx.x << (8 - lanes_shift)) + (threadIdx.x >> lanes_shift); t < n_tokens; t += step) {
     const int64_t token = token_at(tokens, tokens64, t);
@@ -37,15 +37,16 @@ __global__ __launch_bounds__(kThreads) void embedding_kernel(const T* table, int
     const T* from = table + (real ? token * table_stride : 0);
     T* to = out + t * out_stride;
     const int lanes = 1 << lanes_shift;
-    for (int64_t c = (int64_t)(threadIdx.x & (lanes - 1)) * N; c < width; c += (int64_t)lanes * N) {
+    for (int64_t at = (int64_t)(threadIdx.x & (lanes - 1)) * N; at < width; at += (int64_t)lanes * N) {
+      const int64_t c = width < N ? at : min(at, width - N);   // (the last piece's begin is another one's end, with the same values)
       if (c + N <= width) {
         Vec<T, N> v = {};
         if (real) {
-          v = load_vec<T, N>(from + c);
+          v = load_any<T, N>(from + c);
 #pragma unroll
           for (int i = 0; i < N; ++i) v.at[i] = (T)((float)v.at[i] * scale);
         }
-        store_vec<T, N>(to + c, v);
+        store_any<T, N>(to + c, v);
       } else {
         for (int64_t i = c; i < width; ++i) to[i] = real ? (T)((float)from[i] * scale) : (T)0.f;
       }
@@ -333,10 +334,10 @@ template <typename O, int N>
 __device__ __forceinline__ void put_sum(O* out, const float* sum, float scale, int accumulate, int64_t c, int64_t width) {
   if (c + N <= width) {
     Vec<O, N> v = {};
-    if (accumulate) v = load_vec<O, N>(out + c);
+    if (accumulate) v = load_any<O, N>(out + c);
 #pragma unroll
     for (int i = 0; i < N; ++i) v.at[i] = (O)((accumulate ? (float)v.at[i] : 0.f) + sum[i] * scale);
-    store_vec<O, N>(out + c, v);
+    store_any<O, N>(out + c, v);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -386,7 +387,7 @@ __global__ __launch_bounds__(64) void row_sums_kernel(const T* __restrict__ grad
     for (int i = 0; i < kAhead; ++i) {
       const T* from = grad + (int64_t)__builtin_amdgcn_readlane(mine.at, b + i) * grad_stride + c;
       if (whole) {
-        v[i] = load_vec<T, N>(from);
+        v[i] = load_any<T, N>(from);
       } else {
         v[i] = {};
 #pragma unroll
@@ -552,15 +553,10 @@ int fpsched_op_embedding(int device_id, int type, const void* table, int64_t tab
   if (!g.ok) return FPSCHED_EHIP;
   return with_type(type, [&](auto zero) {
     using T = decltype(zero);
-    auto go = [&](auto n) {
-      constexpr int N = decltype(n)::value;
-      const int shift = row_lanes_shift(ceil_div(width, N));
-      embedding_kernel<T, N><<<dim3((unsigned)std::min(kMostGroups, ceil_div(n_tokens, kThreads >> shift))), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
-          static_cast<const T*>(table), table_stride, n_rows, width, tokens, tokens64, n_tokens, scale, static_cast<T*>(out), out_stride, shift);
-      return launched();
-    };
-    if (wide_rows(table, table_stride, sizeof(T)) && wide_rows(out, out_stride, sizeof(T))) return go(std::integral_constant<int, kWide<T>>());
-    return go(std::integral_constant<int, 1>());
+    const int shift = row_lanes_shift(ceil_div(width, kWide<T>));
+    embedding_kernel<T><<<dim3((unsigned)std::min(kMostGroups, ceil_div(n_tokens, kThreads >> shift))), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
+        static_cast<const T*>(table), table_stride, n_rows, width, tokens, tokens64, n_tokens, scale, static_cast<T*>(out), out_stride, shift);
+    return launched();
   });
 }
 
@@ -644,30 +640,24 @@ int fpsched_op_embedding_grad(int device_id, int type, const void* grad, int64_t
       if constexpr (!std::is_same<O, T>::value && !std::is_same<O, float>::value) {
         return (int)FPSCHED_EINVAL;
       } else {
-        auto go = [&](auto n) {
-          constexpr int N = decltype(n)::value;
-          if (w.blocks) {
-            const dim3 blocks((unsigned)w.blocks, (unsigned)ceil_div(width, 64 * N));
-            row_sums_kernel<T, O, N><<<blocks, dim3(64), 0, stream>>>(static_cast<const T*>(grad), grad_stride, width, sorted, total, scale,
-                                                                      static_cast<O*>(out), out_stride, accumulate, parts, w.part_stride);
-            auto join = [&](auto chunks) {
-              for (int64_t at = 0; at < w.blocks; at += kMostGroups)
-                join_runs_kernel<O, N, decltype(chunks)::value><<<dim3((unsigned)std::min(kMostGroups, w.blocks - at), blocks.y), dim3(kJoinWaves * 64), 0, stream>>>(
-                    sorted, total, width, parts, w.part_stride, scale, static_cast<O*>(out), out_stride, accumulate, (unsigned)at);
-            };
-            if (w.blocks > kManyBlocks) {
-              chunk_sums_kernel<N><<<dim3((unsigned)ceil_div(w.blocks, kChunk), blocks.y), dim3(64), 0, stream>>>(sorted, total, width, parts, w.part_stride);
-              join(std::true_type());
-            } else {
-              join(std::false_type());
-            }
+        constexpr int N = kWide<T>;
+        if (w.blocks) {
+          const dim3 blocks((unsigned)w.blocks, (unsigned)ceil_div(width, 64 * N));
+          row_sums_kernel<T, O, N><<<blocks, dim3(64), 0, stream>>>(static_cast<const T*>(grad), grad_stride, width, sorted, total, scale,
+                                                                    static_cast<O*>(out), out_stride, accumulate, parts, w.part_stride);
+          auto join = [&](auto chunks) {
+            for (int64_t at = 0; at < w.blocks; at += kMostGroups)
+              join_runs_kernel<O, N, decltype(chunks)::value><<<dim3((unsigned)std::min(kMostGroups, w.blocks - at), blocks.y), dim3(kJoinWaves * 64), 0, stream>>>(
+                  sorted, total, width, parts, w.part_stride, scale, static_cast<O*>(out), out_stride, accumulate, (unsigned)at);
+          };
+          if (w.blocks > kManyBlocks) {
+            chunk_sums_kernel<N><<<dim3((unsigned)ceil_div(w.blocks, kChunk), blocks.y), dim3(64), 0, stream>>>(sorted, total, width, parts, w.part_stride);
+            join(std::true_type());
+          } else {
+            join(std::false_type());
           }
-          return launched();
-        };
-        // (16 bytes of the gradient a lane, and as many elements of the output: of 32 bits two pieces of 16 bytes)
-        if (wide_rows(grad, grad_stride, sizeof(T)) && aligned(out, sizeof(O) * kWide<T>) && out_stride % kWide<T> == 0)
-          return go(std::integral_constant<int, kWide<T>>());
-        return go(std::integral_constant<int, 1>());
+        }
+        return launched();
       }
     });
   });

@@ -22,6 +22,18 @@ __device__ __forceinline__ void store_vec(T* to, const Vec<T, N>& v) {
   *reinterpret_cast<Vec<T, N>*>(to) = v;
 }
 
+// The same from and to any element's address in global memory (one access of 16 bytes nevertheless).
+template <typename T, int N>
+__device__ __forceinline__ Vec<T, N> load_any(const T* from) {
+  Vec<T, N> v;
+  __builtin_memcpy(&v, from, sizeof(v));
+  return v;
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_any(T* to, const Vec<T, N>& v) {
+  __builtin_memcpy(to, &v, sizeof(v));
+}
+
 // elements of 16 bytes
 template <typename T>
 constexpr int kWide = 16 / (int)sizeof(T);
@@ -54,7 +66,6 @@ constexpr int64_t kMostGroups = (1 << 24) - 1;   // workgroups of 256 along a gr
 inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t round_up(size_t n, size_t to) { return (n + to - 1) / to * to; }
-inline bool wide_rows(const void* p, int64_t stride, int size) { return aligned(p, 16) && (stride * size) % 16 == 0; }
 inline int launched() { return hipGetLastError() == hipSuccess ? FPSCHED_OK : FPSCHED_EHIP; }
 
 // f(T()) with the element type of `type`; FPSCHED_EINVAL for another number

@@ -195,3 +195,33 @@ def test_gradient_where_the_sort_changes(n):
         out = torch.zeros(3000, 16, dtype=out_dtype, device="cuda")
         got = ops.embedding_grad(grad.cuda(), tokens.cuda(), 3000, 0.5, out=out, accumulate=out_dtype == torch.float32)
         oracle.assert_near(got, *oracle.embedding_grad(grad, tokens, 3000, 0.5, out_dtype))
+
+
+def test_lookup_of_more_wide_rows_than_a_grid_has_workgroups():
+    # (a workgroup moves a row of 2,048: 69 GB of them)
+    n, width = (1 << 24) + 83, 2048
+    table = torch.randn(1000, width, device="cuda").half()
+    tokens = torch.arange(n, device="cuda", dtype=torch.int32) % 1003 - 1
+    got = ops.embedding(table, tokens)
+    for first in (0, (1 << 24) - 100, n - 100):
+        at = tokens[first:first + 100].long()
+        want = torch.where(((at >= 0) & (at < 1000))[:, None], table[at.clamp(0, 999)], 0)
+        assert torch.equal(got[first:first + 100], want), first
+    del got
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_at_any_address(dtype):
+    # (rows that begin at any element, of widths around the pieces of 16 bytes; what is beside them stays)
+    for width in (1, 3, 7, 8, 9, 15, 17, 63, 65, 130):
+        for first in (0, 1, 3):
+            store = torch.randn(50, width + first + 2).to(dtype).cuda()
+            table = store[:, first:first + width]
+            tokens = tokens_of(40, 50, width).cuda()
+            got = ops.embedding(table, tokens)
+            oracle.assert_near(got, *oracle.embedding(table.cpu(), tokens.cpu(), 1.0))
+            out = torch.full((50, width + 5), 7.0, dtype=torch.float32, device="cuda")
+            ops.embedding_grad(got, tokens, 50, out=out[:, first:first + width])
+            oracle.assert_near(out[:, first:first + width], *oracle.embedding_grad(got.cpu(), tokens.cpu(), 50, 1.0, torch.float32))
+            assert bool((out[:, :first] == 7).all()) and bool((out[:, first + width:] == 7).all())
