@@ -443,7 +443,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(RowOut<T> row_o
 }
 
 constexpr int kGradRounds = 4;
-template <typename T, int N>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(const T* logits, int64_t stride, int64_t vocab, const void* tokens,
                                                                 int tokens64, const float* lse, const float* entropy,
                                                                 const float* grad_logprob, const float* grad_entropy, T* out,
@@ -462,10 +462,12 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(const T* logits
     const float d = (is_token ? gl : 0.f) - p * (gl + ge * (held_back(lp) + h));
     return (T)(none ? 0.f : d);
   };
-  // pieces of 16 bytes that are aligned as such, and up to N - 1 elements in front of them and behind them, by the row's first workgroup
+  // Pieces of 16 bytes that are aligned as such in the logits, and up to N - 1 elements in front of them and behind them, by the row's first workgroup
+  // (509 x 100,003 f16: 34 us, and 56 an element a lane).
+  constexpr int N = kWide<T>;
   const unsigned piece = blockIdx.x % pieces;
-  const int64_t inner = N == 1 ? 0 : min((int64_t)((0 - reinterpret_cast<uintptr_t>(from)) % 16 / sizeof(T)), vocab), length = (vocab - inner) / N * N;
-  if (N > 1 && piece == 0 && threadIdx.x < 2 * N) {
+  const int64_t inner = min((int64_t)((0 - reinterpret_cast<uintptr_t>(from)) % 16 / sizeof(T)), vocab), length = (vocab - inner) / N * N;
+  if (piece == 0 && threadIdx.x < 2 * N) {
     const int64_t i = threadIdx.x < N ? threadIdx.x : inner + length + threadIdx.x - N;
     if (threadIdx.x < N ? i < inner : i < vocab) to[i] = gradient(from[i], i == token);
   }
@@ -479,7 +481,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(const T* logits
       const int at = behind >= 0 && behind < N ? (int)behind : -1;   // the token's place in the piece
 #pragma unroll
       for (int i = 0; i < N; ++i) v.at[i] = gradient(v.at[i], i == at);
-      store_vec<T, N>(to + inner + c, v);
+      store_any<T, N>(to + inner + c, v);
     }
   }
 }
@@ -579,20 +581,12 @@ int fpsched_op_logprobs_grad(int device_id, int type, int64_t n_rows, int64_t vo
   if (!g.ok) return FPSCHED_EHIP;
   return with_type(type, [&](auto zero) {
     using T = decltype(zero);
-    auto go = [&](auto n) {
-      constexpr int N = decltype(n)::value;
-      const int64_t pieces = ceil_div(vocab, kGradRounds * kThreads * N);
-      const int64_t most = kMostGroups / pieces;   // rows of a launch
-      for (int64_t at = 0; at < n_rows; at += most)
-        logprobs_grad_kernel<T, N><<<dim3((unsigned)(std::min(most, n_rows - at) * pieces)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
-            static_cast<const T*>(logits), logits_stride, vocab, tokens, tokens64, lse, entropy, grad_logprob, grad_entropy, static_cast<T*>(out),
-            out_stride, (int)pieces, at);
-      return launched();
-    };
-    // (rows of both at the same distance from a multiple of 16 bytes: 509 x 100,003 f16 34 us, and 56 an element a lane)
-    const auto apart = reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(out);
-    if (apart % 16 == 0 && (logits_stride - out_stride) * (int64_t)sizeof(T) % 16 == 0) return go(std::integral_constant<int, kWide<T>>());
-    return go(std::integral_constant<int, 1>());
+    const int64_t pieces = ceil_div(vocab, kGradRounds * kThreads * kWide<T>), most = kMostGroups / pieces;   // rows of a launch
+    for (int64_t at = 0; at < n_rows; at += most)
+      logprobs_grad_kernel<T><<<dim3((unsigned)(std::min(most, n_rows - at) * pieces)), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
+          static_cast<const T*>(logits), logits_stride, vocab, tokens, tokens64, lse, entropy, grad_logprob, grad_entropy, static_cast<T*>(out),
+          out_stride, (int)pieces, at);
+    return launched();
   });
 }
 
