@@ -60,7 +60,7 @@ int fpsched_op_embedding_grad(int device_id, int type, const void *grad, int64_t
  * Per sequence and channel, with a = sigmoid(gate):  h[t] = a[t] h[t-1] + (1 - a[t]) value[t], from
  * h[-1] = state (zero if NULL).  out[t] = h[t]; final_state = h at the sequence's end (float; may be
  * the same memory as state).  lengths (int32 [n_batch], NULL: all n_steps; clamped to 0 .. n_steps):
- * behind a sequence's end nothing is read, out is zero and the state stands still.  gate, value, out:
+ * what is behind a sequence's end does not count, out is zero and the state stands still.  gate, value, out:
  * [n_batch][n_steps][width] of `type`, channels adjacent, steps and sequences `strides` elements apart
  * (HOST: batch and step stride of gate, of value, of out; <= 2^31, and of an output no two elements in one place); state, final_state: float [n_batch][width].
  * kept (NULL, or float [n_batch][ceil(n_steps / FPSCHED_RECURRENCE_BLOCK)][width]): the state in front

@@ -199,3 +199,13 @@ def test_many_segments(width):
     assert np.abs(done["out"][0].cpu().double().numpy() - out).max() <= 1e-5
     back = ops.gated_recurrence_grad(grad.cuda(), gate.cuda(), value.cuda(), done["kept"])
     assert np.abs(back["value"][0].cpu().double().numpy() - behind * (1 - a)).max() <= 1e-5 * (1 + np.abs(behind).max())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,steps,width", [(5, 7, 33), (5, 8, 34), (5, 9, 34), (300, 9, 34), (300, 16, 130), (260, 16, 33), (300, 17, 34), (3, 16, 200)])
+def test_few_steps(dtype, n, steps, width):
+    gate, value, grad, state, grad_state = inputs(n, steps, width, dtype, 7)
+    check(gate, value, grad, state, grad_state, None)
+    lengths = torch.randint(0, steps + 1, (n,), generator=torch.Generator().manual_seed(steps), dtype=torch.int32)
+    lengths[0], lengths[1] = 0, steps
+    check(gate, value, grad, state, None, lengths)
