@@ -581,8 +581,8 @@ int fpsched_op_recurrence(int device_id, int type, int64_t n_batch, int64_t n_st
     RecurrenceArgs<T> a = {};
     a.gate = static_cast<const T*>(gate); a.value = static_cast<const T*>(value); a.out = static_cast<T*>(out);
     a.s_gate = {strides[0], strides[1]}; a.s_value = {strides[2], strides[3]}; a.s_out = {strides[4], strides[5]};
-    a.state = state; a.final_state = final_state; a.kept = kept; a.lengths = lengths;
-    a.steps = n_steps; a.width = width;
+    a.state = state; a.final_state = final_state; a.kept = n_steps > 0 ? kept : nullptr;   // (no steps: no blocks, and no room for a state in front of one)
+    a.lengths = lengths; a.steps = n_steps; a.width = width;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return with_channels<T>(width, {gate, value, out}, {strides[0], strides[1], strides[2], strides[3], strides[4], strides[5]}, [&](auto n) {
       constexpr int N = decltype(n)::value;
