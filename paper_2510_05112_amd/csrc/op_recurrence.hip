@@ -528,8 +528,10 @@ void run_walk(RecurrenceArgs<T> a, const Cut& s, int64_t n_batch, unsigned x, fl
   walk(a, dim3(x, (unsigned)n_batch, s.segments));
 }
 
-// Whether no two elements of an output share memory: the steps of a sequence behind one another, or the sequences of a step.
+// Whether no two elements of an output share memory: the steps of a sequence behind one another, or the sequences of a step.  (Of no elements none do,
+// whatever the strides: those of packed sequences of no steps are 0.)
 bool apart(int64_t n_batch, int64_t n_steps, int64_t width, int64_t batch, int64_t step) {
+  if (n_batch == 0 || n_steps == 0 || width == 0) return true;
   if (n_batch <= 1) return n_steps <= 1 || step >= width;
   if (n_steps <= 1) return batch >= width;
   return (step >= width && batch >= (n_steps - 1) * step + width) || (batch >= width && step >= (n_batch - 1) * batch + width);
