@@ -21,7 +21,7 @@ namespace fpsched {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int64_t kMaxWidth = 1 << 20, kMaxSummed = 1 << 30;   // (what the grids have room for: 64 lanes for 16 tokens of a gradient)
+constexpr int64_t kMaxWidth = 1 << 20, kMaxSummed = 1 << 30, kMostRows = 0x7fffffff;   // (places and tokens are 32-bit numbers)
 
 // ---- lookup ----------------------------------------------------------------------------------------------------------
 
@@ -345,14 +345,14 @@ __device__ __forceinline__ void put_sum(O* out, const float* sum, float scale, i
   }
 }
 
-// blockIdx.x: block of sorted occurrences, blockIdx.y: piece of the width.  Part 2 b: of the run that block b begins in
+// blockIdx.x: block of sorted occurrences behind first_block, blockIdx.y: piece of the width.  Part 2 b: of the run that block b begins in
 // the middle of, 2 b + 1: of the run that goes on behind it.
 template <typename T, typename O, int N>
 __global__ __launch_bounds__(64) void row_sums_kernel(const T* __restrict__ grad, int64_t grad_stride, int64_t width,
                                                      const Occurrence* __restrict__ sorted, const unsigned* __restrict__ n, float scale,
                                                      O* __restrict__ out, int64_t out_stride, int accumulate, float* __restrict__ parts,
-                                                     int64_t part_stride) {
-  const unsigned first = blockIdx.x * (unsigned)kBlock, all = *n;
+                                                     int64_t part_stride, unsigned first_block) {
+  const unsigned block = first_block + blockIdx.x, first = block * (unsigned)kBlock, all = *n;
   if (first >= all) return;
   const unsigned end = min(first + kBlock, all);
   // A lane an occurrence, for all lanes to read: lanes behind the width stay, with the first column's addresses, and write nothing (a lane that
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(64) void row_sums_kernel(const T* __restrict__ grad
     } else if (inside && ends) {
       put_sum<O, N>(out + (int64_t)now * out_stride, sum, scale, accumulate, c, width);
     } else {
-      float* part = parts + (2 * (int64_t)blockIdx.x + inside) * part_stride + c;   // (part_stride has room for whole vectors)
+      float* part = parts + (2 * (int64_t)block + inside) * part_stride + c;   // (part_stride has room for whole vectors)
 #pragma unroll
       for (int i = 0; i < N; ++i) part[i] = sum[i];
     }
@@ -561,7 +561,7 @@ int fpsched_op_embedding(int device_id, int type, const void* table, int64_t tab
 }
 
 size_t fpsched_op_embedding_grad_workspace_bytes(int64_t n_rows, int64_t width, int64_t n_tokens) {
-  if (n_rows < 0 || width < 0 || width > kMaxWidth || n_tokens < 0 || n_rows > 0x7ffffffell || n_tokens >= kMaxSummed) return 0;
+  if (n_rows < 0 || width < 0 || width > kMaxWidth || n_tokens < 0 || n_rows > kMostRows || n_tokens >= kMaxSummed) return 0;
   return grad_workspace(width, n_tokens).bytes;
 }
 
@@ -570,7 +570,7 @@ int fpsched_op_embedding_grad(int device_id, int type, const void* grad, int64_t
                               int64_t out_stride, int accumulate, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
   if (type < FPSCHED_BF16 || type > FPSCHED_F32 || (out_type != type && out_type != FPSCHED_F32)) return FPSCHED_EINVAL;
   if (accumulate && out_type != FPSCHED_F32) return FPSCHED_EINVAL;
-  if (n_rows < 0 || width < 0 || width > kMaxWidth || n_tokens < 0 || n_rows > 0x7ffffffell || n_tokens >= kMaxSummed) return FPSCHED_EINVAL;
+  if (n_rows < 0 || width < 0 || width > kMaxWidth || n_tokens < 0 || n_rows > kMostRows || n_tokens >= kMaxSummed) return FPSCHED_EINVAL;
   if (grad_stride < width || out_stride < width) return FPSCHED_EINVAL;
   if (device_id < 0) return FPSCHED_ENODEV;
   if (n_rows == 0 || width == 0) return FPSCHED_OK;
@@ -642,16 +642,17 @@ int fpsched_op_embedding_grad(int device_id, int type, const void* grad, int64_t
       } else {
         constexpr int N = kWide<T>;
         if (w.blocks) {
-          const dim3 blocks((unsigned)w.blocks, (unsigned)ceil_div(width, 64 * N));
-          row_sums_kernel<T, O, N><<<blocks, dim3(64), 0, stream>>>(static_cast<const T*>(grad), grad_stride, width, sorted, total, scale,
-                                                                    static_cast<O*>(out), out_stride, accumulate, parts, w.part_stride);
+          const unsigned pieces = (unsigned)ceil_div(width, 64 * N);
+          for (int64_t at = 0; at < w.blocks; at += kMostWaves)
+            row_sums_kernel<T, O, N><<<dim3((unsigned)std::min(kMostWaves, w.blocks - at), pieces), dim3(64), 0, stream>>>(
+                static_cast<const T*>(grad), grad_stride, width, sorted, total, scale, static_cast<O*>(out), out_stride, accumulate, parts, w.part_stride, (unsigned)at);
           auto join = [&](auto chunks) {
             for (int64_t at = 0; at < w.blocks; at += kMostGroups)
-              join_runs_kernel<O, N, decltype(chunks)::value><<<dim3((unsigned)std::min(kMostGroups, w.blocks - at), blocks.y), dim3(kJoinWaves * 64), 0, stream>>>(
+              join_runs_kernel<O, N, decltype(chunks)::value><<<dim3((unsigned)std::min(kMostGroups, w.blocks - at), pieces), dim3(kJoinWaves * 64), 0, stream>>>(
                   sorted, total, width, parts, w.part_stride, scale, static_cast<O*>(out), out_stride, accumulate, (unsigned)at);
           };
           if (w.blocks > kManyBlocks) {
-            chunk_sums_kernel<N><<<dim3((unsigned)ceil_div(w.blocks, kChunk), blocks.y), dim3(64), 0, stream>>>(sorted, total, width, parts, w.part_stride);
+            chunk_sums_kernel<N><<<dim3((unsigned)ceil_div(w.blocks, kChunk), pieces), dim3(64), 0, stream>>>(sorted, total, width, parts, w.part_stride);
             join(std::true_type());
           } else {
             join(std::false_type());

@@ -61,7 +61,7 @@ struct OpsDevice {   // makes a GPU the current one for a call's launches
   }
 };
 
-constexpr int64_t kMostGroups = (1 << 24) - 1;   // workgroups of 256 along a grid's x, which has room for 2^32 lanes
+constexpr int64_t kMostGroups = (1 << 24) - 1, kMostWaves = (1 << 26) - 1;   // workgroups of 256 and of 64 along a grid's x, which has room for 2^32 - 1 lanes
 
 inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
