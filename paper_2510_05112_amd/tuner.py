@@ -316,8 +316,9 @@ def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_back
     items (``stages.Stage``) are run in turn on one micro-batch and timed.  tokens: [batch][steps] int32 or int64, the first
     stage's input; targets: the last stage's, default tokens.  Returns dict(dur: int32 [8][S] in units of unit_us microseconds, at least
     1 each, for ``Problem``: R and FD cost what F does, B is the whole backward pass without split_backward, O and L are 0;
-    us: float [8][S], the medians of the repeats; kept_bytes: int64 [S], what a stage holds of a micro-batch between its F and
-    its last backward item, for mem_units).  The weights' gradients are as before afterwards."""
+    us: float [8][S], the medians of the repeats; kept_bytes: int64 [S], the most that a stage holds of a micro-batch between two of
+    its items, for mem_units: what F kept and, with split_backward, what B keeps for W beside it).  The weights' gradients are
+    as before afterwards."""
     import torch
 
     from .stages import kept_bytes
@@ -344,10 +345,14 @@ def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_back
                     at_b.record()
                     _, grad_kept = stage.input_grad(grad, kept)
                     at[2].record()
+                    if split_backward:
+                        held[s] = max(held[s], kept_bytes([kept, grad_kept]))   # (the activation is freed behind W)
+                    at_w = torch.cuda.Event(enable_timing=True)
+                    at_w.record()
                     stage.weight_grad(kept, grad_kept)
                     at[3].record()
                     at[3].synchronize()
-                    times.append((at[0].elapsed_time(at[1]), at_b.elapsed_time(at[2]), at[2].elapsed_time(at[3])))
+                    times.append((at[0].elapsed_time(at[1]), at_b.elapsed_time(at[2]), at_w.elapsed_time(at[3])))
                 us[1:4, s] = 1e3 * np.median(np.asarray(times[1:]), axis=0)
                 inputs = out
         finally:
