@@ -11,6 +11,7 @@ left out unless the user asks for it; unit1 = unit2 = 1.
 """
 from __future__ import annotations
 
+import time
 from dataclasses import dataclass
 
 import numpy as np
@@ -311,10 +312,22 @@ def tune_shared(gen_handle, sync_handle, problem, shared_problem, k: int = 8, in
     return [dict(label=labels[int(i)], makespan=int(t), index=int(i), slid=False) for i, t in zip(idx, ms)]
 
 
+def _spin_cycles_per_s(torch):
+    """Cycles of a kernel that only waits, for each second that it takes."""
+    cycles, at = 1 << 20, [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    for _ in range(2):   # (the first: its code is loaded)
+        at[0].record()
+        torch.cuda._sleep(cycles)
+        at[1].record()
+        at[1].synchronize()
+    return 1e3 * cycles / at[0].elapsed_time(at[1])
+
+
 def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_backward: bool = True, repeats: int = 5):
     """The cost table of a model's stages on this GPU, as the paper's profiler (Section 3) delivers it: every stage's F, B and W
-    items (``stages.Stage``) are run in turn on one micro-batch and timed.  tokens: [batch][steps] int32 or int64, the first
-    stage's input; targets: the last stage's, default tokens.  Returns dict(dur: int32 [8][S] in units of unit_us microseconds, at least
+    items (``stages.Stage``) are run in turn on one micro-batch and timed, behind a kernel that waits until the host has enqueued
+    them: a pipeline's host is ahead, and what it takes to launch an item is not part of its cost (but for an item that waits for
+    the GPU itself).  tokens: [batch][steps] int32 or int64, the first stage's input; targets: the last stage's, default tokens.  Returns dict(dur: int32 [8][S] in units of unit_us microseconds, at least
     1 each, for ``Problem``: R and FD cost what F does, B is the whole backward pass without split_backward, O and L are 0;
     us: float [8][S], the medians of the repeats; kept_bytes: int64 [S], the most that a stage holds of a micro-batch between two of
     its items, for mem_units: what F kept and, with split_backward, what B keeps for W beside it).  The weights' gradients are
@@ -330,11 +343,15 @@ def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_back
     us, held = np.zeros((8, len(stages))), np.zeros(len(stages), np.int64)
     inputs = tokens
     with torch.cuda.device(device):
+        cycles_per_s = _spin_cycles_per_s(torch)
         saved = [{name: g.clone() for name, g in layer.grads.items()} for stage in stages for layer in stage.layers if hasattr(layer, "grads")]
         try:
             for s, stage in enumerate(stages):
-                times = []
-                for _ in range(repeats + 1):   # (the first: memory is allocated, code is loaded)
+                times, host = [], 0.0
+                for repeat in range(repeats + 2):   # (the first: memory is allocated, code is loaded; the second: what the host takes)
+                    if repeat > 1:
+                        torch.cuda._sleep(int(cycles_per_s * min(1.5 * host + 1e-4, 1.0)))
+                    began = time.perf_counter()
                     at = [torch.cuda.Event(enable_timing=True) for _ in range(4)]
                     at[0].record()
                     out, kept = stage.forward(inputs, targets)
@@ -351,9 +368,11 @@ def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_back
                     at_w.record()
                     stage.weight_grad(kept, grad_kept)
                     at[3].record()
+                    if repeat > 0:
+                        host = max(host, time.perf_counter() - began)
                     at[3].synchronize()
                     times.append((at[0].elapsed_time(at[1]), at_b.elapsed_time(at[2]), at_w.elapsed_time(at[3])))
-                us[1:4, s] = 1e3 * np.median(np.asarray(times[1:]), axis=0)
+                us[1:4, s] = 1e3 * np.median(np.asarray(times[2:]), axis=0)
                 inputs = out
         finally:
             for layer, grads in zip([x for stage in stages for x in stage.layers if hasattr(x, "grads")], saved):
@@ -363,8 +382,9 @@ def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_back
         us[2] += us[3]
         us[3] = 0
     us[4] = us[7] = us[1]
-    dur = np.where(us > 0, np.maximum(1, np.rint(us / unit_us)), 0).astype(np.int32)
-    return dict(dur=dur, us=us, kept_bytes=held)
+    dur = np.maximum(1, np.rint(us / unit_us))
+    dur[[0, 5, 6] if split_backward else [0, 3, 5, 6]] = 0
+    return dict(dur=dur.astype(np.int32), us=us, kept_bytes=held)
 
 
 def stride_for(problem) -> int:

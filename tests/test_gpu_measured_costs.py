@@ -57,3 +57,35 @@ def test_kept_bytes_are_what_the_allocator_has_handed_out():
         stage.weight_grad(kept, grad_kept)
         del kept, grad_kept
     assert (held_f, held_b) == (by_hand(False)[1], by_hand(True)[1]) and costs["kept_bytes"][1] == held_b
+
+
+class SlowHost(st.Layer):
+    """A layer whose items take the host milliseconds and the GPU microseconds."""
+
+    def work(self, x):
+        time.sleep(0.004)
+        return x + 1
+
+    def forward(self, x):
+        return self.work(x), {}
+
+    def input_grad(self, grad, kept):
+        return self.work(grad), {}
+
+    def weight_grad(self, kept, grad_kept):
+        self.done = self.work(torch.zeros(64, 64, device="cuda"))
+
+
+def test_costs_are_the_gpus_and_not_what_the_host_takes_to_launch():
+    stages = [st.Stage([SlowHost(), SlowHost()]) for _ in range(2)]
+    costs = tuner.measure_costs(stages, torch.zeros(64, 64, device="cuda"), repeats=3)
+    assert costs["us"][1:4].min() > 0 and costs["us"][1:4].max() < 1000, costs["us"]   # (8 ms of the host's)
+
+
+def test_costs_of_items_that_wait_for_the_gpu_themselves():
+    class Waits(SlowHost):
+        def work(self, x):
+            return x + float(x.sum())
+
+    costs = tuner.measure_costs([st.Stage([Waits()])], torch.zeros(64, 64, device="cuda"), repeats=2)
+    assert np.isfinite(costs["us"]).all() and (costs["dur"][1:4] > 0).all()
