@@ -349,6 +349,7 @@ def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_back
             for s, stage in enumerate(stages):
                 times, host = [], 0.0
                 for repeat in range(repeats + 2):   # (the first: memory is allocated, code is loaded; the second: what the host takes)
+                    out = kept = grad = grad_kept = None   # (a stage that fills the memory has room for one micro-batch)
                     if repeat > 1:
                         torch.cuda._sleep(int(cycles_per_s * min(1.5 * host + 1e-4, 1.0)))
                     began = time.perf_counter()

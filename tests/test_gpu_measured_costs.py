@@ -89,3 +89,20 @@ def test_costs_of_items_that_wait_for_the_gpu_themselves():
 
     costs = tuner.measure_costs([st.Stage([Waits()])], torch.zeros(64, 64, device="cuda"), repeats=2)
     assert np.isfinite(costs["us"]).all() and (costs["dur"][1:4] > 0).all()
+
+
+def test_one_micro_batch_is_held_at_a_time():
+    class Large(SlowHost):
+        def forward(self, x):
+            return x + 1, dict(kept=torch.empty(256 << 20, dtype=torch.uint8, device="cuda"))
+
+        def input_grad(self, grad, kept):
+            return grad + 1, dict(kept=torch.empty(128 << 20, dtype=torch.uint8, device="cuda"))
+
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    costs = tuner.measure_costs([st.Stage([Large()]) for _ in range(2)], torch.zeros(64, 64, device="cuda"), repeats=2)
+    assert costs["kept_bytes"].tolist() == [384 << 20] * 2
+    assert torch.cuda.max_memory_allocated() - before < 400 << 20
