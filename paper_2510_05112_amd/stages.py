@@ -17,6 +17,12 @@ def _normal(shape, std, dtype, device, generator):
     return (torch.randn(shape, device=device, generator=generator) * std).to(dtype)
 
 
+def _add_product(total, a, b):
+    """total += a^T b, where total is float32: the products are added to it in 32 bits, without a rounding to their type in between."""
+    import torch
+    torch.addmm(total, a.t(), b, out_dtype=torch.float32, out=total)
+
+
 class Layer:
     """weights and grads: dicts of tensors by the same names, the latter float32 and zero until a ``weight_grad``."""
 
@@ -67,7 +73,7 @@ class Recurrence(Layer):
 
     def weight_grad(self, kept, grad_kept):
         width = self.weights["w"].shape[1]
-        self.grads["w"] += grad_kept["both"].reshape(-1, 2 * width).t() @ kept["x"].reshape(-1, width)
+        _add_product(self.grads["w"], grad_kept["both"].reshape(-1, 2 * width), kept["x"].reshape(-1, width))
 
 
 class FeedForward(Layer):
@@ -117,7 +123,7 @@ class Head(Layer):
         return (d @ self.weights["w"]).view(kept["shape"]), dict(logits=d)
 
     def weight_grad(self, kept, grad_kept):
-        self.grads["w"] += grad_kept["logits"].t() @ kept["x"]
+        _add_product(self.grads["w"], grad_kept["logits"], kept["x"])
 
 
 class Stage:
