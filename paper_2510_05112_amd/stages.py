@@ -61,7 +61,7 @@ class Recurrence(Layer):
         return both[..., :width], both[..., width:]
 
     def forward(self, x):
-        both = (x.reshape(-1, x.shape[-1]) @ self.weights["w"].t()).view(*x.shape[:-1], -1)
+        both = (x.reshape(-1, x.shape[-1]) @ self.weights["w"].t()).view(*x.shape[:-1], len(self.weights["w"]))
         done = stage_ops.gated_recurrence(*self._halves(both), keep=True)
         return x + done["out"], dict(x=x, both=both, states=done["kept"])
 

@@ -59,3 +59,20 @@ def test_weight_gradients_beyond_float16(kind):
     layer.grads["w"].zero_()
     items(layer, torch.full((1, n), 2.0 ** -14, device="cuda").half(), torch.full((1, 16), 2.0 ** -14, device="cuda").half())
     assert bool((layer.grads["w"] == 2.0 ** -28).all())
+
+
+@pytest.mark.parametrize("batch,steps", [(0, 5), (3, 0), (0, 0)])
+def test_a_micro_batch_of_no_tokens(batch, steps):
+    """(A shard of a batch that has none.)  Nothing is added to the gradients."""
+    model = st.language_model(2, 2, 64, 96, 500)
+    tokens = torch.zeros(batch, steps, dtype=torch.int64, device="cuda")
+    x, kept0 = model[0].forward(tokens)
+    loss, kept1 = model[1].forward(x, tokens)
+    assert x.shape == (batch, steps, 64) and float(loss) == 0
+    grad, grad_kept1 = model[1].input_grad(1.0, kept1)
+    assert grad.shape == x.shape
+    none, grad_kept0 = model[0].input_grad(grad, kept0)
+    assert none is None
+    for stage, kept, grad_kept in zip(model, (kept0, kept1), (grad_kept0, grad_kept1)):
+        stage.weight_grad(kept, grad_kept)
+        assert not any(bool(g.any()) for layer in stage.layers for g in layer.grads.values())
