@@ -176,11 +176,11 @@ def embedding_grad(grad, tokens, rows: int, scale: float = 1.0, out=None, accumu
     rows = int(rows)
     if rows < 0:
         raise ValueError("rows: not negative")
-    if grad.dim() < 2 or grad.shape[:-1] != tokens.shape:
+    if grad.dim() < 1 or grad.shape[:-1] != tokens.shape:
         raise ValueError("grad: one row for every token")
     _tensor(grad, "grad", device, dtypes=_TYPES, rows=grad.dim() == 2)
     width = grad.shape[-1]
-    flat = grad if grad.dim() == 2 else grad.reshape(-1, width)
+    flat = grad if grad.dim() == 2 else grad.view(tokens.numel(), width)
     if accumulate and (out is None or out.dtype != torch.float32):
         raise ValueError("accumulate: needs a float32 out")
     with _Stream(stream, device) as s:

@@ -20,3 +20,19 @@ def test_gradient_of_the_most_tokens():
     assert torch.equal(got[:, 0], want.float())
     del tokens, grad, got, want
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("shape", [(), (1,), (5,), (2, 3), (0, 4), (2, 3, 2)])
+@pytest.mark.parametrize("width", [0, 1, 40])
+def test_tokens_of_any_shape_both_ways(shape, width):
+    rows = 7
+    table = torch.randn(rows, width, device="cuda")
+    tokens = torch.randint(0, rows, shape, device="cuda")
+    got = ops.embedding(table, tokens)
+    assert got.shape == (*shape, width) and torch.equal(got, table[tokens])
+    grad = torch.ones_like(got)
+    back = ops.embedding_grad(grad, tokens, rows)
+    want = torch.bincount(tokens.reshape(-1), minlength=rows)[:, None].float().expand(rows, width)
+    assert back.shape == (rows, width) and torch.equal(back, want)
+    added = ops.embedding_grad(grad, tokens, rows, out=back.clone(), accumulate=True)
+    assert torch.equal(added, 2 * want)
