@@ -40,6 +40,7 @@ class Embedding(Layer):
         self.scale = math.sqrt(width)
 
     def forward(self, tokens):
+        tokens = tokens.contiguous()   # (a text's tokens but the last are a view)
         return stage_ops.embedding(self.weights["table"], tokens, self.scale), dict(tokens=tokens)
 
     def input_grad(self, grad, kept):

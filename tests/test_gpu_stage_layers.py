@@ -4,6 +4,7 @@ import torch
 
 import stage_oracle as oracle
 from paper_2510_05112_amd import stages as st
+from paper_2510_05112_amd import tuner
 
 pytestmark = pytest.mark.gpu
 
@@ -76,3 +77,21 @@ def test_a_micro_batch_of_no_tokens(batch, steps):
     for stage, kept, grad_kept in zip(model, (kept0, kept1), (grad_kept0, grad_kept1)):
         stage.weight_grad(kept, grad_kept)
         assert not any(bool(g.any()) for layer in stage.layers for g in layer.grads.values())
+
+
+def test_tokens_that_are_views():
+    # (a text's tokens but the last, and those behind each)
+    model = st.language_model(2, 2, 64, 96, 500)
+    text = torch.randint(0, 500, (3, 41), device="cuda")
+    tokens, targets = text[:, :-1], text[:, 1:]
+    for of, to in ((tokens, targets), (tokens.t(), targets.t())):
+        x, kept0 = model[0].forward(of)
+        want, _ = model[0].forward(of.contiguous())
+        assert torch.equal(x, want)
+        loss, kept1 = model[1].forward(x, to)
+        assert torch.equal(loss, model[1].forward(want, to.contiguous())[0])
+        grad, _ = model[1].input_grad(1.0, kept1)
+        _, grad_kept0 = model[0].input_grad(grad, kept0)
+        model[0].weight_grad(kept0, grad_kept0)
+    costs = tuner.measure_costs(model, tokens, targets, repeats=1)
+    assert (costs["dur"][1:4] > 0).all()
