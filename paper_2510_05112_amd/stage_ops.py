@@ -294,10 +294,11 @@ def _activation(name):
 
 
 def _kept_views(room, tokens, hidden, dtype):
-    """The memory that a feed-forward block keeps, as the B item leaves it: d_pre and hidden."""
+    """The memory that a feed-forward block keeps, as the B item leaves it: d_pre and hidden.  item: whose numbers they are, "F" or "B", in a
+    list that copies of the dict share."""
     both = room.view(dtype)
     n = 2 * tokens * hidden
-    return dict(pre=both[:n].view(tokens, 2 * hidden), hidden=both[n:].view(tokens, hidden))
+    return dict(pre=both[:n].view(tokens, 2 * hidden), hidden=both[n:].view(tokens, hidden), item=["F"])
 
 
 def _kept_memory(kept, tokens, hidden, dtype, device):
@@ -307,6 +308,11 @@ def _kept_memory(kept, tokens, hidden, dtype, device):
     if h.untyped_storage().data_ptr() != pre.untyped_storage().data_ptr() or h.data_ptr() != pre.data_ptr() + 4 * tokens * hidden:
         raise ValueError("kept: not the memory that gated_ffn returned")
     return pre
+
+
+def _kept_item(kept):
+    """Whose numbers are kept.  (Views that were put together anew do not say.)"""
+    return kept["item"][0] if "item" in kept else None
 
 
 def gated_ffn(x, w_in, w_out, activation: str = "silu", keep: bool = False, out=None, workspace=None, stream=None):
@@ -332,18 +338,22 @@ def gated_ffn(x, w_in, w_out, activation: str = "silu", keep: bool = False, out=
 
 def gated_ffn_input_grad(grad, w_in, w_out, kept, activation: str = "silu", workspace=None, stream=None):
     """The B item: the gradient of x from that of the output and what ``gated_ffn`` kept.  Returns dict(x, kept: what
-    ``gated_ffn_weight_grad`` needs).  It takes the place of what was kept: this is called once for each ``gated_ffn``."""
+    ``gated_ffn_weight_grad`` needs).  It takes the place of what was kept: this is called once for each ``gated_ffn`` (ValueError)."""
     device = _device(grad, "grad")
     tokens, width, hidden = _ffn_sizes(grad, "grad", w_in, w_out, device)
     act = _activation(activation)
     memory = _kept_memory(kept, tokens, hidden, grad.dtype, device)
+    if _kept_item(kept) == "B":
+        raise ValueError("kept: gated_ffn_input_grad has taken its place, once for each gated_ffn")
     _rows_of_16_bytes(grad=grad, w_in=w_in, w_out=w_out, kept=memory)
     with _Stream(stream, device) as s:
         d_x = s.empty(tokens, width, dtype=grad.dtype)
         room = s.room(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
         s.call("ffn_input_grad", _TYPES[grad.dtype], act, tokens, width, hidden, grad.data_ptr(), _matrix_stride(grad), w_in.data_ptr(),
                w_out.data_ptr(), memory.data_ptr(), d_x.data_ptr(), width, *room)
-    return dict(x=d_x, kept=dict(pre=kept["pre"], hidden=kept["hidden"]))
+    if "item" in kept:
+        kept["item"][0] = "B"
+    return dict(x=d_x, kept={name: kept[name] for name in ("pre", "hidden", "item") if name in kept})
 
 
 def gated_ffn_weight_grad(x, grad, kept, grad_kept, out=None, accumulate: bool = False, workspace=None, stream=None):
@@ -360,6 +370,8 @@ def gated_ffn_weight_grad(x, grad, kept, grad_kept, out=None, accumulate: bool =
     memory = _kept_memory(grad_kept, tokens, hidden, x.dtype, device)
     if kept["pre"].data_ptr() != memory.data_ptr():
         raise ValueError("grad_kept: of another call than kept")
+    if _kept_item(grad_kept) == "F":
+        raise ValueError("grad_kept: gated_ffn_input_grad comes first")
     if accumulate and (out is None or out["w_in"].dtype != torch.float32):
         raise ValueError("accumulate: needs float32 outputs")
     with _Stream(stream, device) as s:
