@@ -11,7 +11,7 @@ split the way the items are split:
 ``tuner.measure_costs`` times stages made of them.  As elsewhere in the package the functions only check and marshal arguments: CUDA
 tensors in, CUDA tensors out, asynchronous on ``stream`` (default: the device's current one), on the GPU the tensors are on
 whether or not that is the current one.  What is not handed in (``out``, ``workspace``) is allocated on that stream.  The
-gradients are calls of their own; autograd takes no part.  Wrong arguments raise ``ValueError``, what the library refuses ``FpschedError``.
+gradients are calls of their own; autograd takes no part: an output never requires a gradient, also where an input does.  Wrong arguments raise ``ValueError``, what the library refuses ``FpschedError``.
 """
 from __future__ import annotations
 
@@ -294,11 +294,12 @@ def _activation(name):
 
 
 def _kept_views(room, tokens, hidden, dtype):
-    """The memory that a feed-forward block keeps, as the B item leaves it: d_pre and hidden.  item: whose numbers they are, "F" or "B", in a
-    list that copies of the dict share."""
+    """The memory that a feed-forward block keeps, as the B item leaves it: d_pre and hidden."""
     both = room.view(dtype)
     n = 2 * tokens * hidden
-    return dict(pre=both[:n].view(tokens, 2 * hidden), hidden=both[n:].view(tokens, hidden), item=["F"])
+    pre = both[:n].view(tokens, 2 * hidden)
+    pre.numbers_of = "F"   # (the item whose numbers are in that memory: copies of the dict share the tensor)
+    return dict(pre=pre, hidden=both[n:].view(tokens, hidden))
 
 
 def _kept_memory(kept, tokens, hidden, dtype, device):
@@ -310,15 +311,16 @@ def _kept_memory(kept, tokens, hidden, dtype, device):
     return pre
 
 
-def _kept_item(kept):
-    """Whose numbers are kept.  (Views that were put together anew do not say.)"""
-    return kept["item"][0] if "item" in kept else None
+def _kept_item(memory):
+    """Whose numbers are kept.  (Views that a caller has made do not say.)"""
+    return getattr(memory, "numbers_of", None)
 
 
 def gated_ffn(x, w_in, w_out, activation: str = "silu", keep: bool = False, out=None, workspace=None, stream=None):
     """(act(x w_gate^T) * (x w_up^T)) w_out^T, with w_in = [w_gate; w_up].  x: [tokens][width], rows any distance apart; w_in: [2
-    hidden][width]; w_out: [width][hidden]; bfloat16 or float16; widths multiples of 8.  Returns dict(out, kept: with ``keep``,
-    what the two gradients need, six bytes for each token and hidden channel)."""
+    hidden][width]; w_out: [width][hidden]; bfloat16 or float16; widths multiples of 8.  Between the products hidden is rounded to that
+    type, and so is what ``gated_ffn_input_grad`` multiplies by w_in.  Returns dict(out, kept: with ``keep``, what the two gradients
+    need, six bytes for each token and hidden channel)."""
     device = _device(x, "x")
     tokens, width, hidden = _ffn_sizes(x, "x", w_in, w_out, device)
     act = _activation(activation)
@@ -343,7 +345,7 @@ def gated_ffn_input_grad(grad, w_in, w_out, kept, activation: str = "silu", work
     tokens, width, hidden = _ffn_sizes(grad, "grad", w_in, w_out, device)
     act = _activation(activation)
     memory = _kept_memory(kept, tokens, hidden, grad.dtype, device)
-    if _kept_item(kept) == "B":
+    if _kept_item(memory) == "B":
         raise ValueError("kept: gated_ffn_input_grad has taken its place, once for each gated_ffn")
     _rows_of_16_bytes(grad=grad, w_in=w_in, w_out=w_out, kept=memory)
     with _Stream(stream, device) as s:
@@ -351,9 +353,8 @@ def gated_ffn_input_grad(grad, w_in, w_out, kept, activation: str = "silu", work
         room = s.room(workspace, _lib().fpsched_op_ffn_workspace_bytes(tokens, width, hidden))
         s.call("ffn_input_grad", _TYPES[grad.dtype], act, tokens, width, hidden, grad.data_ptr(), _matrix_stride(grad), w_in.data_ptr(),
                w_out.data_ptr(), memory.data_ptr(), d_x.data_ptr(), width, *room)
-    if "item" in kept:
-        kept["item"][0] = "B"
-    return dict(x=d_x, kept={name: kept[name] for name in ("pre", "hidden", "item") if name in kept})
+    memory.numbers_of = "B"
+    return dict(x=d_x, kept=dict(pre=kept["pre"], hidden=kept["hidden"]))
 
 
 def gated_ffn_weight_grad(x, grad, kept, grad_kept, out=None, accumulate: bool = False, workspace=None, stream=None):
@@ -370,7 +371,7 @@ def gated_ffn_weight_grad(x, grad, kept, grad_kept, out=None, accumulate: bool =
     memory = _kept_memory(grad_kept, tokens, hidden, x.dtype, device)
     if kept["pre"].data_ptr() != memory.data_ptr():
         raise ValueError("grad_kept: of another call than kept")
-    if _kept_item(grad_kept) == "F":
+    if _kept_item(memory) == "F":
         raise ValueError("grad_kept: gated_ffn_input_grad comes first")
     if accumulate and (out is None or out["w_in"].dtype != torch.float32):
         raise ValueError("accumulate: needs float32 outputs")
@@ -394,7 +395,8 @@ def token_logprobs(logits, tokens, alternatives: int = 0, workspace=None, stream
     vocabulary, -1 for padding: log probability 0).  Returns dict(logprob, entropy: float32 [rows], lse: float32 [rows][2], the log-sum-exp in
     two parts (largest logit, rest), and with ``alternatives`` = k > 0 the k largest logits of each row, of equal ones the
     lowest id first, as ids: int32 [rows][k] and logprobs: float32 [rows][k]; -1 and -inf where fewer are not masked).  A logit of
-    -inf is masked; a row with nothing else has logprob -inf and entropy 0; one with NaN or +inf is NaN throughout."""
+    -inf is masked; a row with nothing else has logprob -inf and entropy 0; one with NaN or +inf, padding or not, is NaN
+    throughout (of lse, the rest)."""
     device = _device(logits, "logits")
     if logits.dim() != 2 or not logits.shape[1]:
         raise ValueError("logits: [rows][vocab]")

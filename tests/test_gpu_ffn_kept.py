@@ -58,3 +58,11 @@ def test_layers_out_of_order():
         layer.input_grad(grad, kept)
     layer.weight_grad(kept, grad_kept)
     assert st.kept_bytes(kept) == 2 * x.numel() + 6 * 40 * 72   # (x, and g and u in 24 bits)
+
+
+def test_what_is_kept_is_tensors_alone():
+    x, w_in, w_out, grad = block()
+    kept = ops.gated_ffn(x, w_in, w_out, keep=True)["kept"]
+    back = ops.gated_ffn_input_grad(grad, w_in, w_out, kept)["kept"]
+    for held in (kept, back):
+        assert set(held) == {"pre", "hidden"} and all(torch.is_tensor(t) for t in held.values())
