@@ -19,7 +19,8 @@
  * may share a workspace, or a tensor that one of them writes, only if they run one after the other.
  * Workspaces are 16-byte aligned, tensors to their elements.  A size of 0 rows is no error: nothing is read, and what is
  * written of a gradient over no rows is zero.  Sums, states and softmax statistics are held in 32
- * bits; an output of a 16-bit type is rounded once, to nearest even.  Results are the same bits
+ * bits; an output of a 16-bit type is rounded once, to nearest even, and nothing on the way to it is rounded to fewer than 32
+ * bits but for what the feed-forward block says below.  Results are the same bits
  * from call to call (no atomic decides an order of additions).
  */
 #ifndef FPSCHED_OPS_H
@@ -38,7 +39,7 @@ enum { FPSCHED_BF16 = 0, FPSCHED_F16 = 1, FPSCHED_F32 = 2 };
  * out[t][:] = scale * table[tokens[t]][:].  A token outside 0 .. n_rows - 1 (-1 for padding) gives
  * zeros, and no row of the table is read for it.  table: [n_rows][width], rows table_stride elements
  * apart (>= width); out: [n_tokens][width], rows out_stride apart, of the same type; tokens int32 or,
- * with tokens64, int64.  width <= 2^20. */
+ * with tokens64, int64.  width <= 2^20, n_tokens < 2^31. */
 int fpsched_op_embedding(int device_id, int type, const void *table, int64_t table_stride, int64_t n_rows,
                          int64_t width, const void *tokens, int tokens64, int64_t n_tokens, float scale,
                          void *out, int64_t out_stride, void *hip_stream);
@@ -49,7 +50,7 @@ int fpsched_op_embedding(int device_id, int type, const void *table, int64_t tab
  * written, with zeros where no token is; with accumulate (out_type FPSCHED_F32 only) the sums are added
  * to what out holds, and rows without a token are left as they are.  grad: [n_tokens][width] of `type`,
  * rows grad_stride apart; out: [n_rows][width] of `type` or FPSCHED_F32, rows out_stride apart.
- * n_tokens < 2^30, n_rows < 2^31. */
+ * width <= 2^20, n_tokens < 2^30, n_rows < 2^31. */
 size_t fpsched_op_embedding_grad_workspace_bytes(int64_t n_rows, int64_t width, int64_t n_tokens);
 int fpsched_op_embedding_grad(int device_id, int type, const void *grad, int64_t grad_stride, int64_t n_rows,
                               int64_t width, const void *tokens, int tokens64, int64_t n_tokens, float scale,
@@ -65,7 +66,7 @@ int fpsched_op_embedding_grad(int device_id, int type, const void *grad, int64_t
  * (HOST: batch and step stride of gate, of value, of out; <= 2^31, and of an output no two elements in one place); state, final_state: float [n_batch][width].
  * kept (NULL, or float [n_batch][ceil(n_steps / FPSCHED_RECURRENCE_BLOCK)][width]): the state in front
  * of every block of steps, from which the backward pass starts.  One step (n_steps = 1) is the form for
- * serving.  n_batch < 2^16, width <= 2^24. */
+ * serving.  n_batch < 2^16, n_steps < 2^31, width <= 2^24. */
 #define FPSCHED_RECURRENCE_BLOCK 64
 size_t fpsched_op_recurrence_workspace_bytes(int64_t n_batch, int64_t n_steps, int64_t width);
 int fpsched_op_recurrence(int device_id, int type, int64_t n_batch, int64_t n_steps, int64_t width,
@@ -89,8 +90,11 @@ int fpsched_op_recurrence_grad(int device_id, int type, int64_t n_batch, int64_t
  * hidden: [n_tokens][hidden_width], free again when the call's work is done; kept: NULL, or
  * FPSCHED_FFN_KEPT_BYTES of g and u in 24 bits for the backward pass.  Types FPSCHED_BF16 and FPSCHED_F16, the
  * same for all; weights and hidden contiguous.  width, hidden_width and the strides are multiples of 8,
- * the tensors 16-byte aligned (FPSCHED_EINVAL): rows are moved 16 bytes at a time.  act is computed in 32
- * bits from unrounded g and u.  FPSCHED_EUNSUPPORTED where a product has 2^23 tiles of 128 x 128 or more. */
+ * the tensors 16-byte aligned (FPSCHED_EINVAL): rows are moved 16 bytes at a time; width and strides <= 2^21,
+ * hidden_width <= 2^20, n_tokens < 2^31.  act is computed in 32
+ * bits from unrounded g and u; hidden is rounded to `type`, as the matrix cores take it, for the second product, which is as much
+ * of an error again as rounding out is (as are d_pre and hidden for the gradients).  FPSCHED_EUNSUPPORTED where a product has 2^23
+ * tiles of 128 x 128 or more. */
 enum { FPSCHED_SILU = 0, FPSCHED_GELU = 1 /* with tanh */, FPSCHED_RELU = 2 };
 #define FPSCHED_FFN_KEPT_BYTES(n_tokens, hidden_width) ((size_t)6 * (n_tokens) * (hidden_width))
 size_t fpsched_op_ffn_workspace_bytes(int64_t n_tokens, int64_t width, int64_t hidden_width);
@@ -122,7 +126,7 @@ int fpsched_op_ffn_weight_grad(int device_id, int type, int64_t n_tokens, int64_
  * rest, for the backward pass.  A logit of minus infinity is masked: probability 0, and no alternative (id
  * -1, log probability minus infinity).  A row with nothing else: logprob minus infinity, entropy 0,
  * lse (0, minus infinity).  A token outside 0 .. vocab - 1 (-1 for padding): logprob 0.  A row that holds
- * NaN or plus infinity: NaN throughout, ids -1.  vocab >= 1, n_rows < 2^31, vocab < 2^31. */
+ * NaN or plus infinity, padding or not: NaN throughout (of lse, the rest), ids -1.  vocab >= 1, n_rows < 2^31, vocab < 2^31. */
 size_t fpsched_op_logprobs_workspace_bytes(int64_t n_rows, int64_t vocab, int n_alternatives);
 int fpsched_op_logprobs(int device_id, int type, int64_t n_rows, int64_t vocab, const void *logits,
                         int64_t logits_stride, const void *tokens, int tokens64, int n_alternatives,
