@@ -135,8 +135,8 @@ int fpsched_op_logprobs(int device_id, int type, int64_t n_rows, int64_t vocab, 
 
 /* The gradient of the logits for the gradients of logprob and of entropy (either may be NULL: zero):
  *   out[i] = grad_logprob ([i = token] - p[i]) - grad_entropy p[i] (log p[i] + entropy).
- * A row without a valid token takes no grad_logprob; a row with every logit masked gets zeros.  out has
- * the logits' type and may be the same memory (with the same stride). */
+ * A row without a valid token takes no grad_logprob; a row with every logit masked gets zeros.  A p below
+ * 2^-126 counts as 0.  out has the logits' type and may be the same memory (with the same stride). */
 int fpsched_op_logprobs_grad(int device_id, int type, int64_t n_rows, int64_t vocab, const void *logits,
                              int64_t logits_stride, const void *tokens, int tokens64, const float *lse,
                              const float *entropy, const float *grad_logprob, const float *grad_entropy,

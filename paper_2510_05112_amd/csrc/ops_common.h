@@ -42,7 +42,7 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, int tokens64, in
   return tokens64 ? static_cast<const int64_t*>(tokens)[i] : (int64_t)static_cast<const int32_t*>(tokens)[i];
 }
 
-// exp and log by the hardware's base-2 forms (an error of about 2^-23 in the result, 2^-24 times the argument in exp's)
+// exp and log by the hardware's base-2 forms (an error of about 2^-23 in the result, 2^-24 times the argument in exp's; what exp gives below 2^-126 is 0)
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
 __device__ __forceinline__ float fast_log(float x) { return __logf(x); }
 
