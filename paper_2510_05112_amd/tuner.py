@@ -351,7 +351,7 @@ def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_back
                 for repeat in range(repeats + 2):   # (the first: memory is allocated, code is loaded; the second: what the host takes)
                     out = kept = grad = grad_kept = None   # (a stage that fills the memory has room for one micro-batch)
                     if repeat > 1:
-                        torch.cuda._sleep(int(cycles_per_s * min(1.5 * host + 1e-4, 1.0)))
+                        torch.cuda._sleep(int(cycles_per_s * min(2 * host + 1e-4, 1.0)))
                     began = time.perf_counter()
                     at = [torch.cuda.Event(enable_timing=True) for _ in range(4)]
                     at[0].record()
@@ -369,8 +369,8 @@ def measure_costs(stages, tokens, targets=None, unit_us: float = 1.0, split_back
                     at_w.record()
                     stage.weight_grad(kept, grad_kept)
                     at[3].record()
-                    if repeat > 0:
-                        host = max(host, time.perf_counter() - began)
+                    if repeat == 1:   # (later ones may wait for the waiting kernel)
+                        host = time.perf_counter() - began
                     at[3].synchronize()
                     times.append((at[0].elapsed_time(at[1]), at_b.elapsed_time(at[2]), at_w.elapsed_time(at[3])))
                 us[1:4, s] = 1e3 * np.median(np.asarray(times[2:]), axis=0)

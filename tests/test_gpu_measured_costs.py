@@ -106,3 +106,17 @@ def test_one_micro_batch_is_held_at_a_time():
     costs = tuner.measure_costs([st.Stage([Large()]) for _ in range(2)], torch.zeros(64, 64, device="cuda"), repeats=2)
     assert costs["kept_bytes"].tolist() == [384 << 20] * 2
     assert torch.cuda.max_memory_allocated() - before < 400 << 20
+
+
+def test_items_that_wait_for_the_gpu_do_not_wait_longer_each_time():
+    class Waits(SlowHost):
+        times = []
+
+        def work(self, x):
+            self.times.append(time.perf_counter())
+            torch.cuda.current_stream().synchronize()
+            return x + 1
+
+    tuner.measure_costs([st.Stage([Waits()])], torch.zeros(64, 64, device="cuda"), repeats=16)
+    # (16 repeats behind a waiting kernel of a fraction of a millisecond; of half as much again each time, they would take half a second)
+    assert Waits.times[-1] - Waits.times[6] < 0.1
